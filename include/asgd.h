@@ -10,6 +10,7 @@
  *     asgd_apply_update  (the server applies a pushed gradient)
  *     asgd_apply_update_snapshot (push and the same replica's next fetch, fused)
  *     asgd_train_step    (gradient, push and fetch of one replica, pipelined by layer)
+ *     asgd_apply_update_clipped, asgd_train_step_clipped (the push bounded by the gradient's norm)
  * plus the calls that describe the network and the on-one-GPU A-SGD replay.
  *
  * Conventions
@@ -376,6 +377,67 @@ int asgd_replay_nsync_run(asgd_net_t *const *nets, int n_workers, int n_sync, fl
  * or accum + grads, device fp32 [n].
  * Errors: ASGD_EINVAL (null with n > 0), ASGD_EALIGN, ASGD_EHIP. */
 int asgd_accumulate(float *accum, const float *grads, size_t n, int first, void *stream);
+
+/* ---- gradients bounded by their norm --------------------------------------
+ * A replica that is several updates old can push a gradient that is far too
+ * large for the parameters it meets.  norm = sqrt(sum of g^2) over all elements
+ * of all tensors; a gradient is clipped to max_norm by the factor
+ * min(1, max_norm / norm).  A gradient that holds an infinity or a NaN is
+ * clipped to zero everywhere, and the norm reports it.
+ *   grads, counts : host arrays of n_tensors device pointers and element counts
+ *             (a pointer may be null where the count is 0); copied by the call.
+ *             Tensors need only the alignment of their elements: the slices of a
+ *             flat vector that asgd_param_layout names are ordinary arguments.
+ *             A tensor that is listed twice counts twice.
+ *   dtype   : ASGD_F32 or ASGD_BF16, of all tensors.
+ *   norm    : device, 1 float; overwritten with the norm before clipping.
+ *             asgd_grad_norm needs it, the others take null for "not wanted".
+ *             (A finite gradient whose norm is beyond fp32's range reports an
+ *             infinity and is clipped all the same.)
+ *   workspace : device, asgd_grad_norm_workspace_bytes(n_tensors) bytes, 16-byte
+ *             aligned; written before it is read, so its contents do not matter.
+ *             Calls that may overlap on the GPU need one each.
+ * Squares are summed in 64 bits, in a fixed order. */
+size_t asgd_grad_norm_workspace_bytes(int n_tensors);
+/* Errors: ASGD_EINVAL (null, negative count of tensors, unknown dtype),
+ * ASGD_EALIGN, ASGD_EHIP. */
+int asgd_grad_norm(const void *const *grads, const size_t *counts, int n_tensors, int dtype,
+                   float *norm, void *workspace, void *stream);
+
+/* The clipped gradient: clipped[i] = factor * grads[i], rounded to the tensors'
+ * type (ties to even).
+ *   clipped  : host array of n_tensors device pointers, where the clipped
+ *             tensors go: grads[i] itself (in place; nothing is written where
+ *             the norm is within max_norm) or memory that overlaps no gradient
+ *             and no other clipped tensor.
+ *   max_norm : > 0; an infinity clips nothing.
+ * Errors: as asgd_grad_norm; ASGD_EINVAL for a max_norm that is not > 0 and for
+ * overlapping tensors; ASGD_ENOMEM (host). */
+int asgd_clip_grads(const void *const *grads, void *const *clipped, const size_t *counts,
+                    int n_tensors, int dtype, float max_norm, float *norm, void *workspace,
+                    void *stream);
+
+/* The server's update for a pushed gradient that is clipped to max_norm on the
+ * way: asgd_clip_grads on grads (one fp32 tensor), then asgd_apply_update with
+ * the clipped gradient, or asgd_apply_update_snapshot where worker_copy is not
+ * null, bit for bit, without the clipped gradient in memory; grads stay as they
+ * are.  workspace: of asgd_grad_norm_workspace_bytes(1).
+ * Errors: as asgd_apply_update_snapshot and asgd_clip_grads. */
+int asgd_apply_update_clipped(float *params, float *momentum, const float *grads, size_t n,
+                              float lr, float mu, float wd, float max_norm, void *worker_copy,
+                              int dst_dtype, float *norm, void *workspace, void *stream);
+
+/* asgd_fwd_bwd on `worker_copy`, then asgd_apply_update_clipped of the whole
+ * gradient with the replica's next fetch: the cycle of asgd_train_step with the
+ * push bounded.  (Which parameters move how far is known only when the whole
+ * gradient is, so no layer is pushed before.)  grads hold the gradient before
+ * clipping; the result is that of the two calls, bit for bit.
+ * Errors: as asgd_train_step and asgd_apply_update_clipped. */
+int asgd_train_step_clipped(asgd_net_t *net, float *master, float *momentum, void *worker_copy,
+                            const void *images, const int32_t *labels, uint64_t dropout_seed,
+                            uint64_t step, uint32_t worker, float *loss, float *grads, float lr,
+                            float mu, float wd, float max_norm, float *norm, void *workspace,
+                            void *stream);
 
 /* Text of the last error on the calling thread ("" if none). */
 const char *asgd_last_error(void);

@@ -21,6 +21,7 @@ EXPORTS = ["asgd_net_create", "asgd_net_prepare", "asgd_net_destroy", "asgd_net_
            "asgd_apply_update", "asgd_snapshot",
            "asgd_apply_update_snapshot", "asgd_train_step", "asgd_train_step_fused",
            "asgd_debug_get", "asgd_profile_begin", "asgd_profile_end", "asgd_schedule_generate", "asgd_replay_run", "asgd_replay_nsync_run", "asgd_accumulate", "asgd_apply_update_adagrad", "asgd_apply_update_adadelta",
+           "asgd_grad_norm_workspace_bytes", "asgd_grad_norm", "asgd_clip_grads", "asgd_apply_update_clipped", "asgd_train_step_clipped",
            "asgd_last_error"]
 KERNEL_CLASSES = ["conv_fwd", "conv_dgrad", "conv_wgrad", "fc_fwd", "fc_dgrad", "fc_wgrad", "pool_fwd", "pool_bwd",
                   "bias_grad", "softmax_ce", "layout", "update", "lrn"]
@@ -94,6 +95,14 @@ def lib():
         L.asgd_accumulate.argtypes = [vp, vp, ctypes.c_size_t, ctypes.c_int, vp]
         L.asgd_apply_update_adagrad.argtypes = [vp, vp, vp, ctypes.c_size_t, ctypes.c_float, ctypes.c_float, ctypes.c_float, vp]
         L.asgd_apply_update_adadelta.argtypes = [vp, vp, vp, vp, ctypes.c_size_t, ctypes.c_float, ctypes.c_float, ctypes.c_float, vp]
+        L.asgd_grad_norm_workspace_bytes.argtypes = [ctypes.c_int]
+        L.asgd_grad_norm_workspace_bytes.restype = ctypes.c_size_t
+        L.asgd_grad_norm.argtypes = [vp, vp, ctypes.c_int, ctypes.c_int, vp, vp, vp]
+        L.asgd_clip_grads.argtypes = [vp, vp, vp, ctypes.c_int, ctypes.c_int, ctypes.c_float, vp, vp, vp]
+        L.asgd_apply_update_clipped.argtypes = [vp, vp, vp, ctypes.c_size_t, ctypes.c_float, ctypes.c_float, ctypes.c_float, ctypes.c_float, vp,
+                                                ctypes.c_int, vp, vp, vp]
+        L.asgd_train_step_clipped.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.c_uint64, ctypes.c_uint64, ctypes.c_uint32, vp, vp, ctypes.c_float,
+                                              ctypes.c_float, ctypes.c_float, ctypes.c_float, vp, vp, vp]
         L.asgd_last_error.restype = ctypes.c_char_p
         _lib = L
     return _lib
@@ -292,3 +301,47 @@ def asgd_apply_update_adagrad(params, hist, grads, lr, eps, wd, stream=None, n=N
 def asgd_apply_update_adadelta(params, avg_sq_grad, avg_sq_step, grads, rho, eps, wd, stream=None, n=None):
     _check(lib().asgd_apply_update_adadelta(_ptr(params), _ptr(avg_sq_grad), _ptr(avg_sq_step), _ptr(grads),
                                             params.numel() if n is None else n, rho, eps, wd, _stream(stream)))
+
+
+class TensorList:
+    """Device pointers and element counts of a list of tensors, for callers that pass the same tensors again and again."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.n = len(self.tensors)
+        self.ptrs = (ctypes.c_void_p * self.n)(*[t.data_ptr() for t in self.tensors])
+        self.counts = (ctypes.c_size_t * self.n)(*[t.numel() for t in self.tensors])
+
+
+def _tensors(ts):
+    return ts if isinstance(ts, TensorList) else TensorList(ts)
+
+
+def asgd_grad_norm_workspace_bytes(n_tensors):
+    return int(lib().asgd_grad_norm_workspace_bytes(n_tensors))
+
+
+def asgd_grad_norm(grads, dtype, norm, workspace, stream=None):
+    """grads: a list of device tensors, or a TensorList of them."""
+    g = _tensors(grads)
+    _check(lib().asgd_grad_norm(g.ptrs, g.counts, g.n, dtype, _ptr(norm), _ptr(workspace), _stream(stream)))
+
+
+def asgd_clip_grads(grads, clipped, dtype, max_norm, norm, workspace, stream=None):
+    """grads, clipped: lists of as many device tensors of the same sizes (or TensorLists); the same list for both clips in place."""
+    g = _tensors(grads)
+    c = g if clipped is grads else _tensors(clipped)
+    if c.n != g.n or (c is not g and bytes(c.counts) != bytes(g.counts)):
+        raise ValueError("asgd_clip_grads: the clipped tensors have other sizes than the gradients")
+    _check(lib().asgd_clip_grads(g.ptrs, c.ptrs, g.counts, g.n, dtype, max_norm, _ptr(norm), _ptr(workspace), _stream(stream)))
+
+
+def asgd_apply_update_clipped(params, momentum, grads, lr, mu, wd, max_norm, worker_copy, dst_dtype, norm, workspace, stream=None, n=None):
+    _check(lib().asgd_apply_update_clipped(_ptr(params), _ptr(momentum), _ptr(grads), params.numel() if n is None else n, lr, mu, wd, max_norm,
+                                           _ptr(worker_copy), dst_dtype, _ptr(norm), _ptr(workspace), _stream(stream)))
+
+
+def asgd_train_step_clipped(net, master, momentum, worker_copy, images, labels, dropout_seed, step, worker, loss, grads, lr, mu, wd, max_norm, norm,
+                            workspace, stream=None):
+    _check(lib().asgd_train_step_clipped(net, _ptr(master), _ptr(momentum), _ptr(worker_copy), _ptr(images), _ptr(labels), dropout_seed, step, worker,
+                                         _ptr(loss), _ptr(grads), lr, mu, wd, max_norm, _ptr(norm), _ptr(workspace), _stream(stream)))

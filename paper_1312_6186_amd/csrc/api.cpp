@@ -1674,4 +1674,125 @@ int asgd_accumulate(float *accum, const float *grads, size_t n, int first, void 
     return ASGD_OK;
 }
 
+// ---- gradients bounded by their norm
+namespace {
+// What all calls over many tensors check.  out may be null (the norm alone).
+int check_tensors(const char *name, const void *const *grads, void *const *out, const size_t *counts, int n, int dtype, const float *norm, const void *workspace)
+{
+    if (n < 0) return fail(ASGD_EINVAL, "%s: negative number of tensors", name);
+    if (dtype != ASGD_F32 && dtype != ASGD_BF16) return fail(ASGD_EINVAL, "%s: unknown dtype %d", name, dtype);
+    if (!workspace) return fail(ASGD_EINVAL, "%s: null workspace", name);
+    if (((uintptr_t)workspace & 15) || ((uintptr_t)norm & 3)) return fail(ASGD_EALIGN, "%s: the workspace must be 16-byte aligned, norm 4-byte", name);
+    if (n > 0 && (!grads || !counts)) return fail(ASGD_EINVAL, "%s: null argument", name);
+    const size_t es = dtype_size(dtype);
+    for (int i = 0; i < n; ++i) {
+        if (counts[i] == 0) continue;
+        if (!grads[i] || (out && !out[i])) return fail(ASGD_EINVAL, "%s: tensor %d is null", name, i);
+        if (((uintptr_t)grads[i] | (uintptr_t)(out ? out[i] : nullptr)) & (es - 1)) return fail(ASGD_EALIGN, "%s: tensor %d is not aligned to its elements", name, i);
+        if (counts[i] > ((size_t)1 << 46) / es) return fail(ASGD_EINVAL, "%s: tensor %d is too large", name, i);
+    }
+    return ASGD_OK;
+}
+
+// Whether a clipped tensor overlaps another one, or a gradient that is not its own.
+bool clipped_overlap(const void *const *grads, void *const *out, const size_t *counts, int n, size_t es)
+{
+    struct Span { uintptr_t begin, end; bool written; };
+    std::vector<Span> spans;
+    spans.reserve(2 * (size_t)n);
+    bool sorted = true;
+    auto add = [&](const void *p, size_t count, bool written) {
+        const uintptr_t b = (uintptr_t)p;
+        if (!spans.empty() && b < spans.back().begin) sorted = false;
+        spans.push_back({b, b + count * es, written});
+    };
+    for (int i = 0; i < n; ++i)
+        if (counts[i]) add(out[i], counts[i], true);
+    for (int i = 0; i < n; ++i)
+        if (counts[i] && grads[i] != out[i]) add(grads[i], counts[i], false);
+    if (!sorted) std::sort(spans.begin(), spans.end(), [](const Span &a, const Span &b) { return a.begin < b.begin; });
+    uintptr_t end = 0, written_end = 0;   // of everything, and of what is written, so far
+    for (const Span &s : spans) {
+        if (s.written ? s.begin < end : s.begin < written_end) return true;
+        end = std::max(end, s.end);
+        if (s.written) written_end = std::max(written_end, s.end);
+    }
+    return false;
+}
+}  // namespace
+
+size_t asgd_grad_norm_workspace_bytes(int n_tensors) { return norm_partials(n_tensors > 0 ? n_tensors : 0) * sizeof(double); }
+
+int asgd_grad_norm(const void *const *grads, const size_t *counts, int n_tensors, int dtype, float *norm, void *workspace, void *stream)
+{
+    const int rc = check_tensors("asgd_grad_norm", grads, nullptr, counts, n_tensors, dtype, norm, workspace);
+    if (rc != ASGD_OK) return rc;
+    if (!norm) return fail(ASGD_EINVAL, "asgd_grad_norm: null norm");
+    if (launch_grad_norm(grads, counts, n_tensors, dtype, norm, static_cast<double *>(workspace), static_cast<hipStream_t>(stream)) != 0)
+        return hip_fail(hipGetLastError(), "norm kernels");
+    return ASGD_OK;
+}
+
+int asgd_clip_grads(const void *const *grads, void *const *clipped, const size_t *counts, int n_tensors, int dtype, float max_norm, float *norm,
+                    void *workspace, void *stream)
+{
+    if (n_tensors > 0 && !clipped) return fail(ASGD_EINVAL, "asgd_clip_grads: null argument");
+    const int rc = check_tensors("asgd_clip_grads", grads, clipped, counts, n_tensors, dtype, norm, workspace);
+    if (rc != ASGD_OK) return rc;
+    if (!(max_norm > 0.f)) return fail(ASGD_EINVAL, "asgd_clip_grads: max_norm must be > 0");
+    try {
+        if (clipped_overlap(grads, clipped, counts, n_tensors, dtype_size(dtype))) return fail(ASGD_EINVAL, "asgd_clip_grads: a clipped tensor overlaps another tensor");
+    } catch (const std::bad_alloc &) {
+        return fail(ASGD_ENOMEM, "asgd_clip_grads: out of host memory");
+    }
+    if (launch_clip(grads, clipped, counts, n_tensors, dtype, max_norm, norm, static_cast<double *>(workspace), static_cast<hipStream_t>(stream)) != 0)
+        return hip_fail(hipGetLastError(), "clipping kernels");
+    return ASGD_OK;
+}
+
+namespace {
+int check_update_clipped(const char *name, const float *norm, const void *workspace, float max_norm)
+{
+    if (!workspace) return fail(ASGD_EINVAL, "%s: null workspace", name);
+    if (!(max_norm > 0.f)) return fail(ASGD_EINVAL, "%s: max_norm must be > 0", name);
+    if (((uintptr_t)workspace & 15) || ((uintptr_t)norm & 3)) return fail(ASGD_EALIGN, "%s: the workspace must be 16-byte aligned, norm 4-byte", name);
+    return ASGD_OK;
+}
+}  // namespace
+
+int asgd_apply_update_clipped(float *params, float *momentum, const float *grads, size_t n, float lr, float mu, float wd, float max_norm, void *worker_copy,
+                              int dst_dtype, float *norm, void *workspace, void *stream)
+{
+    if (dst_dtype != ASGD_F32 && dst_dtype != ASGD_BF16) return fail(ASGD_EINVAL, "asgd_apply_update_clipped: unknown dtype %d", dst_dtype);
+    const int rc = check_update_clipped("asgd_apply_update_clipped", norm, workspace, max_norm);
+    if (rc != ASGD_OK) return rc;
+    if (n > 0 && (!params || !momentum || !grads)) return fail(ASGD_EINVAL, "asgd_apply_update_clipped: null argument");
+    if ((((uintptr_t)params | (uintptr_t)momentum | (uintptr_t)grads) & 3) || ((uintptr_t)worker_copy & (dst_dtype == ASGD_BF16 ? 1 : 3)))
+        return fail(ASGD_EALIGN, "asgd_apply_update_clipped: misaligned buffer");
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    double *ws = static_cast<double *>(workspace);
+    const int lrc = n > 0 ? launch_update_clipped(params, momentum, grads, n, lr, mu, wd, max_norm, norm, worker_copy, dst_dtype, ws, st)
+                          : norm ? launch_grad_norm(nullptr, nullptr, 0, ASGD_F32, norm, ws, st) : 0;
+    if (lrc != 0) return hip_fail(hipGetLastError(), "clipped update kernels");
+    return ASGD_OK;
+}
+
+int asgd_train_step_clipped(asgd_net_t *net, float *master, float *momentum, void *worker_copy, const void *images, const int32_t *labels,
+                            uint64_t dropout_seed, uint64_t step, uint32_t worker, float *loss, float *grads, float lr, float mu, float wd, float max_norm,
+                            float *norm, void *workspace, void *stream)
+{
+    if (!master || !momentum) return fail(ASGD_EINVAL, "asgd_train_step_clipped: null argument");
+    if (((uintptr_t)master | (uintptr_t)momentum) & 15) return fail(ASGD_EALIGN, "asgd_train_step_clipped: master and momentum must be 16-byte aligned");
+    int rc = check_update_clipped("asgd_train_step_clipped", norm, workspace, max_norm);
+    if (rc != ASGD_OK) return rc;
+    rc = fwd_bwd(net, worker_copy, images, labels, dropout_seed, step, worker, loss, grads, stream, nullptr);
+    if (rc != ASGD_OK) return rc;
+    const size_t P = net->param_count;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    ProfScope ps(net, st, ASGD_K_UPDATE, 0, (double)P * (24.0 + dtype_size(net->dtype)));
+    if (launch_update_clipped(master, momentum, grads, P, lr, mu, wd, max_norm, norm, worker_copy, net->dtype, static_cast<double *>(workspace), st) != 0)
+        return hip_fail(hipGetLastError(), "clipped update kernels");
+    return ASGD_OK;
+}
+
 }  // extern "C"

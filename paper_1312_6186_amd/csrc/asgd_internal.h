@@ -203,6 +203,21 @@ int launch_push_ranges(PushRanges &p, hipStream_t s);
 // Adagrad / Adadelta server updates (one pass, in place)
 int launch_adagrad(float *w, float *h, const float *g, size_t n, float lr, float eps, float wd, hipStream_t s);
 int launch_adadelta(float *w, float *a, float *b, const float *g, size_t n, float rho, float eps, float wd, hipStream_t s);
+// Norms over many tensors, clipping and clipped updates (clip.hip).  The tensors travel as a kernel argument, kTableTensors a launch.
+constexpr int kTableTensors = 128;
+struct TensorTable {
+    const void *in[kTableTensors]; void *out[kTableTensors];
+    uint64_t count[kTableTensors];          // elements, none of them 0
+    unsigned start[kTableTensors + 1];      // first tile of each, and the number of all
+    int n;
+};
+static_assert(sizeof(TensorTable) <= 3840, "a kernel's arguments have 4 KiB");
+size_t norm_partials(int n_tensors);        // doubles of workspace
+int launch_grad_norm(const void *const *grads, const size_t *counts, int n, int dtype, float *norm, double *partials, hipStream_t s);
+int launch_clip(const void *const *grads, void *const *out, const size_t *counts, int n, int dtype, float max_norm, float *norm, double *partials, hipStream_t s);
+// copy may be null (no snapshot); n > 0
+int launch_update_clipped(float *w, float *v, const float *g, size_t n, float lr, float mu, float wd, float max_norm, float *norm, void *copy, int dst_dtype,
+                          double *partials, hipStream_t s);
 // acc = g (first) or acc + g
 int launch_accumulate(float *acc, const float *g, size_t n, bool first, hipStream_t s);
 int launch_snapshot(const float *src, void *dst, size_t n, int dst_dtype, const int *version_counter,

@@ -1,0 +1,338 @@
+// The norm of a gradient over all of its tensors, gradients clipped to a norm, and the server's update with a clipped gradient.
+//
+//   norm = sqrt(sum over all tensors of g^2),   factor = min(1, max_norm / norm),   clipped = factor * g
+//
+// A gradient that holds an infinity or a NaN has no direction to keep: its clipped form is zero everywhere, and the norm says why.
+//
+// Bound by memory: the norm reads the gradient once; clipping and the update have to know it before they touch the first element, so
+// they read the gradient a second time, from the memory-side cache as far as it still holds it (the second pass runs from the end,
+// where the first one stopped).  Squares are added up in 64 bits, which cannot overflow or lose small elements beside large ones and
+// costs two instructions an element where memory leaves room for fifteen.  Every workgroup of the first pass leaves one sum; every workgroup
+// of the second adds all of them up in the same order before it starts, which saves a launch between the two and gives the same factor
+// everywhere, the same in every run.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "asgd_internal.h"
+#include "stream.h"
+
+namespace asgd {
+
+// A tensor is cut into tiles of 1024 aligned 16-byte pieces, counted from the piece that holds its first element (tensors are slices of a
+// vector: they start and end anywhere).  Each thread takes four pieces of a tile.
+constexpr int kTilePieces = 1024;
+constexpr int kClipBlocks = 2048;   // eight workgroups of four waves a CU
+
+static inline uint64_t tensor_tiles(const void *p, size_t count, int es)
+{
+    if (count == 0) return 0;
+    const uint64_t pieces = (((uintptr_t)p & 15) + (uint64_t)count * es + 15) / 16;
+    return (pieces + kTilePieces - 1) / kTilePieces;
+}
+
+template <typename T> struct Piece {
+    static constexpr int E = 16 / (int)sizeof(T);
+    union { uint4 u; T e[E]; };
+};
+
+// The four pieces of tile `tile` of tensor q that belong to this thread, elements outside the tensor as zeros.  body(piece, first element, whole).
+template <typename T, class F> __device__ __forceinline__ void each_piece(const TensorTable &t, int q, unsigned tile, F &&body)
+{
+    constexpr int E = Piece<T>::E;
+    const uintptr_t addr = reinterpret_cast<uintptr_t>(t.in[q]);
+    const long head = (long)(addr & 15) / (long)sizeof(T), count = (long)t.count[q];
+    const T *base = reinterpret_cast<const T *>(addr & ~(uintptr_t)15);
+    const long first = (long)tile * kTilePieces + threadIdx.x;
+    Piece<T> v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const long at = (first + u * 256) * E - head;   // element of the tensor at the piece's start
+        if (at >= 0 && at + E <= count) {
+            v[u].u = *reinterpret_cast<const uint4 *>(base + (first + u * 256) * E);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const bool in = at + e >= 0 && at + e < count;
+                v[u].e[e] = (T)0.f;
+                if (in) v[u].e[e] = base[(first + u * 256) * E + e];
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const long at = (first + u * 256) * E - head;
+        body(v[u], at, at >= 0 && at + E <= count);
+    }
+}
+
+// The sum of one double a thread over the 256 threads of a workgroup, the same in all of them.
+__device__ __forceinline__ double block_sum(double s, double (&lds)[4])
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+    __syncthreads();
+    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+__device__ __forceinline__ double sum_partials(const double *partials, int n, double (&lds)[4])
+{
+    double s = 0;
+    for (int i = threadIdx.x; i < n; i += 256) s += partials[i];
+    return block_sum(s, lds);
+}
+
+// The factor stays in 64 bits: in 32 it would be short of digits (or zero) for gradients beyond fp32's range, and a clipped element would be rounded twice.
+struct Factor { double f; bool drop; };   // drop: the gradient is not finite
+__device__ __forceinline__ Factor clip_factor(double squares, float max_norm)
+{
+    const double norm = __builtin_sqrt(squares);
+    Factor r;
+    r.drop = !(squares < __builtin_inf());
+    r.f = norm > (double)max_norm ? (double)max_norm / norm : 1.0;
+    return r;
+}
+__device__ __forceinline__ float clipped(float g, const Factor &f) { return f.drop ? 0.f : (float)((double)g * f.f); }
+
+__device__ __forceinline__ int tensor_of(const TensorTable &t, unsigned tile)   // start[q] <= tile < start[q + 1]
+{
+    int lo = 0, hi = t.n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (t.start[mid] <= tile) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+template <typename T> __global__ __launch_bounds__(256) void square_sums_kernel(TensorTable t, double *partials)
+{
+    __shared__ double lds[4];
+    const unsigned tiles = t.start[t.n];
+    const unsigned begin = (unsigned)((uint64_t)tiles * blockIdx.x / gridDim.x), end = (unsigned)((uint64_t)tiles * (blockIdx.x + 1) / gridDim.x);
+    double s = 0;
+    if (begin < end) {
+        int q = tensor_of(t, begin);
+        for (unsigned tile = begin; tile < end; ++tile) {
+            while (tile >= t.start[q + 1]) ++q;
+            each_piece<T>(t, q, tile - t.start[q], [&](const Piece<T> &v, long, bool) ASGD_INLINE {
+#pragma unroll
+                for (int e = 0; e < Piece<T>::E; ++e) {
+                    const double x = (double)ldf(&v.e[e]);
+                    s = __builtin_fma(x, x, s);
+                }
+            });
+        }
+    }
+    s = block_sum(s, lds);
+    if (threadIdx.x == 0) partials[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(256) void norm_kernel(const double *partials, int n, float *norm)
+{
+    __shared__ double lds[4];
+    const double s = sum_partials(partials, n, lds);
+    if (threadIdx.x == 0) *norm = (float)__builtin_sqrt(s);
+}
+
+template <typename T> __global__ __launch_bounds__(256) void clip_kernel(TensorTable t, const double *partials, int n, float max_norm, float *norm)
+{
+    constexpr int E = Piece<T>::E;
+    __shared__ double lds[4];
+    const double squares = sum_partials(partials, n, lds);
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)__builtin_sqrt(squares);
+    const Factor f = clip_factor(squares, max_norm);
+    const bool same = !f.drop && f.f == 1.0;
+    const unsigned tiles = t.start[t.n], back = gridDim.x - 1 - blockIdx.x;   // the last tiles first
+    const unsigned begin = (unsigned)((uint64_t)tiles * back / gridDim.x), end = (unsigned)((uint64_t)tiles * (back + 1) / gridDim.x);
+    if (begin >= end) return;
+    int q = tensor_of(t, end - 1);
+    for (unsigned tile = end; tile-- > begin;) {
+        while (tile < t.start[q]) --q;
+        if (same && t.in[q] == t.out[q]) continue;   // clipped in place by a factor of one
+        T *out = static_cast<T *>(t.out[q]);
+        const bool aligned = ((reinterpret_cast<uintptr_t>(t.in[q]) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
+        const long count = (long)t.count[q];
+        each_piece<T>(t, q, tile - t.start[q], [&](Piece<T> v, long at, bool whole) ASGD_INLINE {
+#pragma unroll
+            for (int e = 0; e < E; ++e) stf(&v.e[e], clipped(ldf(&v.e[e]), f));
+            if (whole && aligned) {
+                *reinterpret_cast<uint4 *>(out + at) = v.u;
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (at + e >= 0 && at + e < count) out[at + e] = v.e[e];
+            }
+        });
+    }
+}
+
+// The update of asgd_apply_update with the clipped gradient, and the new parameters to `copy` (SNAP as in update_kernel): a tile is 1024
+// 16-byte vectors of each buffer.
+template <int SNAP, bool ONCE>
+__global__ __launch_bounds__(256) void clipped_update_kernel(float *w, float *v, const float *g, size_t n, unsigned tiles, float lr, float mu, float wd,
+                                                             const double *partials, int n_partials, float max_norm, float *norm, void *copy)
+{
+    __shared__ double lds[4];
+    const double squares = sum_partials(partials, n_partials, lds);
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)__builtin_sqrt(squares);
+    const Factor f = clip_factor(squares, max_norm);
+    const size_t n4 = n / 4;
+    f32x4 *w4 = reinterpret_cast<f32x4 *>(w), *v4 = reinterpret_cast<f32x4 *>(v);
+    const f32x4 *g4 = reinterpret_cast<const f32x4 *>(g);
+    for (unsigned tile = tiles - 1 - blockIdx.x; tile < tiles; tile -= gridDim.x) {   // below zero it wraps around
+        const size_t i0 = (size_t)tile * 1024 + threadIdx.x;
+        f32x4 ww[4], vv[4], gg[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const size_t i = i0 + u * 256;
+            if (i < n4) { ww[u] = load4<ONCE>(&w4[i]); vv[u] = load4<ONCE>(&v4[i]); gg[u] = __builtin_nontemporal_load(&g4[i]); }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const size_t i = i0 + u * 256;
+            if (i >= n4) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float wn = ww[u][e], vn = vv[u][e];
+                update1(wn, vn, clipped(gg[u][e], f), lr, mu, wd);
+                ww[u][e] = wn; vv[u][e] = vn;
+            }
+            __builtin_nontemporal_store(ww[u], &w4[i]);
+            __builtin_nontemporal_store(vv[u], &v4[i]);
+            if constexpr (SNAP == 1) static_cast<f32x4 *>(copy)[i] = ww[u];
+            if constexpr (SNAP == 2) static_cast<uint2 *>(copy)[i] = bf16x4(ww[u]);
+        }
+    }
+    if (blockIdx.x == 0) {
+        const size_t i = n4 * 4 + threadIdx.x;
+        if (i < n) {
+            float wn = w[i], vn = v[i];
+            update1(wn, vn, clipped(g[i], f), lr, mu, wd);
+            v[i] = vn; w[i] = wn;
+            if constexpr (SNAP == 1) static_cast<float *>(copy)[i] = wn;
+            if constexpr (SNAP == 2) static_cast<uint16_t *>(copy)[i] = (uint16_t)f32_to_bf16_bits(__float_as_uint(wn));
+        }
+    }
+}
+// The same where a buffer is not aligned to its vectors.
+template <int SNAP>
+__global__ __launch_bounds__(256) void clipped_update_scalar_kernel(float *w, float *v, const float *g, size_t n, float lr, float mu, float wd,
+                                                                    const double *partials, int n_partials, float max_norm, float *norm, void *copy)
+{
+    __shared__ double lds[4];
+    const double squares = sum_partials(partials, n_partials, lds);
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)__builtin_sqrt(squares);
+    const Factor f = clip_factor(squares, max_norm);
+    const size_t stride = (size_t)gridDim.x * 256;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += stride) {
+        float wn = w[i], vn = v[i];
+        update1(wn, vn, clipped(g[i], f), lr, mu, wd);
+        v[i] = vn; w[i] = wn;
+        if constexpr (SNAP == 1) static_cast<float *>(copy)[i] = wn;
+        if constexpr (SNAP == 2) static_cast<uint16_t *>(copy)[i] = (uint16_t)f32_to_bf16_bits(__float_as_uint(wn));
+    }
+}
+
+// ---- host side
+
+size_t norm_partials(int n_tensors) { return (size_t)kClipBlocks + (size_t)(n_tensors + kTableTensors - 1) / kTableTensors; }
+
+// Calls launch(table, workgroups, their first partial sum) for every kTableTensors tensors; the number of partial sums, or -1.
+// Workgroups are dealt out by the tables' tiles, at least one a table.
+template <class F> static long each_table(const void *const *in, void *const *out, const size_t *counts, int n, int dtype, F &&launch)
+{
+    const int es = (int)dtype_size(dtype);
+    uint64_t total = 0;
+    for (int i = 0; i < n; ++i) {
+        total += tensor_tiles(in[i], counts[i], es);
+        if (total > 0xffffffffu) return -1;
+    }
+    long first = 0;
+    for (int i = 0; i < n;) {
+        TensorTable t;
+        uint64_t tiles = 0;
+        t.n = 0;
+        for (; i < n && t.n < kTableTensors; ++i) {
+            if (counts[i] == 0) continue;
+            t.in[t.n] = in[i]; t.out[t.n] = out ? out[i] : nullptr; t.count[t.n] = counts[i]; t.start[t.n] = (unsigned)tiles;
+            tiles += tensor_tiles(in[i], counts[i], es);
+            ++t.n;
+        }
+        if (t.n == 0) continue;
+        t.start[t.n] = (unsigned)tiles;
+        const uint64_t share = total > (uint64_t)kClipBlocks ? tiles * kClipBlocks / total : tiles;
+        const unsigned blocks = (unsigned)(share ? share : 1);
+        launch(t, blocks, first);
+        if (launch_ok() != 0) return -1;
+        first += blocks;
+    }
+    return first;
+}
+
+static long launch_square_sums(const void *const *grads, const size_t *counts, int n, int dtype, double *partials, hipStream_t s)
+{
+    return each_table(grads, nullptr, counts, n, dtype, [&](const TensorTable &t, unsigned blocks, long first) {
+        if (dtype == kBF16) hipLaunchKernelGGL(square_sums_kernel<bf16_t>, dim3(blocks), dim3(256), 0, s, t, partials + first);
+        else hipLaunchKernelGGL(square_sums_kernel<float>, dim3(blocks), dim3(256), 0, s, t, partials + first);
+    });
+}
+
+int launch_grad_norm(const void *const *grads, const size_t *counts, int n, int dtype, float *norm, double *partials, hipStream_t s)
+{
+    const long np = launch_square_sums(grads, counts, n, dtype, partials, s);
+    if (np < 0) return -1;
+    hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(256), 0, s, partials, (int)np, norm);
+    return launch_ok();
+}
+
+int launch_clip(const void *const *grads, void *const *out, const size_t *counts, int n, int dtype, float max_norm, float *norm, double *partials, hipStream_t s)
+{
+    const long np = launch_square_sums(grads, counts, n, dtype, partials, s);
+    if (np < 0) return -1;
+    if (np == 0) {
+        if (!norm) return 0;
+        hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(256), 0, s, partials, 0, norm);
+        return launch_ok();
+    }
+    return each_table(grads, out, counts, n, dtype, [&](const TensorTable &t, unsigned blocks, long first) {
+        float *to = first == 0 ? norm : nullptr;
+        if (dtype == kBF16) hipLaunchKernelGGL(clip_kernel<bf16_t>, dim3(blocks), dim3(256), 0, s, t, partials, (int)np, max_norm, to);
+        else hipLaunchKernelGGL(clip_kernel<float>, dim3(blocks), dim3(256), 0, s, t, partials, (int)np, max_norm, to);
+    }) < 0 ? -1 : 0;
+}
+
+template <int SNAP>
+static int launch_update_clipped_t(float *w, float *v, const float *g, size_t n, float lr, float mu, float wd, float max_norm, float *norm, void *copy,
+                                   const double *partials, int np, hipStream_t s)
+{
+    const unsigned copy_align = SNAP == 1 ? 15u : SNAP == 2 ? 7u : 0u;
+    const bool aligned = (((uintptr_t)w | (uintptr_t)v | (uintptr_t)g) & 15) == 0 && ((uintptr_t)copy & copy_align) == 0;
+    if (aligned) {
+        const size_t tiles = (n / 4 + 1023) / 1024;
+        if (tiles > 0x7fffffffu) return -1;
+        const unsigned blocks = (unsigned)std::max<size_t>(1, std::min<size_t>(tiles, kClipBlocks));
+        const auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, s, w, v, g, n, (unsigned)tiles, lr, mu, wd, partials, np, max_norm, norm, copy);
+        };
+        if (beyond_cache(n, 2, SNAP == 1 ? 4 : SNAP == 2 ? 2 : 0)) go(clipped_update_kernel<SNAP, true>);
+        else go(clipped_update_kernel<SNAP, false>);
+    } else {
+        const unsigned blocks = (unsigned)std::min<size_t>((n + 255) / 256, 8192);
+        hipLaunchKernelGGL(clipped_update_scalar_kernel<SNAP>, dim3(blocks), dim3(256), 0, s, w, v, g, n, lr, mu, wd, partials, np, max_norm, norm, copy);
+    }
+    return launch_ok();
+}
+
+int launch_update_clipped(float *w, float *v, const float *g, size_t n, float lr, float mu, float wd, float max_norm, float *norm, void *copy, int dst_dtype,
+                          double *partials, hipStream_t s)
+{
+    const void *grads[1] = {g};
+    const long np = launch_square_sums(grads, &n, 1, kF32, partials, s);
+    if (np < 0) return -1;
+    if (!copy) return launch_update_clipped_t<0>(w, v, g, n, lr, mu, wd, max_norm, norm, nullptr, partials, (int)np, s);
+    if (dst_dtype == kBF16) return launch_update_clipped_t<2>(w, v, g, n, lr, mu, wd, max_norm, norm, copy, partials, (int)np, s);
+    return launch_update_clipped_t<1>(w, v, g, n, lr, mu, wd, max_norm, norm, copy, partials, (int)np, s);
+}
+
+}  // namespace asgd

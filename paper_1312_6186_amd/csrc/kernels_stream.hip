@@ -12,16 +12,9 @@
 #include "asgd_internal.h"
 #include "mfma_common.h"
 #include "reduce.h"
+#include "stream.h"
 
 namespace asgd {
-
-__device__ inline float ldf(const float *p) { return *p; }
-__device__ inline float ldf(const bf16_t *p) { return (float)*p; }
-__device__ inline void stf(float *p, float v) { *p = v; }
-__device__ inline void stf(bf16_t *p, float v) { *p = (bf16_t)v; }
-
-static inline unsigned blocks_for(size_t n, unsigned per_block) { return (unsigned)((n + per_block - 1) / per_block); }
-static inline int launch_ok() { return hipGetLastError() == hipSuccess ? 0 : -1; }
 
 uint64_t dropout_key(uint64_t seed, uint64_t step, uint32_t worker, uint32_t layer)
 {
@@ -29,30 +22,14 @@ uint64_t dropout_key(uint64_t seed, uint64_t step, uint32_t worker, uint32_t lay
 }
 
 // ---------------------------------------------------------------- update
-// t = g + wd*w; v = mu*v - lr*t; w = w + v.  20 bytes of traffic per parameter.
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
+// t = g + wd*w; v = mu*v - lr*t; w = w + v (update1).  20 bytes of traffic per parameter.
+//
 // Each thread owns 4 float4 per buffer, 256 apart, all loads issued before the arithmetic; gradients are read and
 // parameters / momentum written with non-temporal hints (the 1.2 GB working set of the AlexNet-style net cannot
 // stay in cache between steps anyway).  Measured 5.65 TB/s on 62.4 M parameters.
-// One element of the update, with the contractions written out so that every code path (vector body, scalar
-// tail, unaligned fallback) rounds identically: t = g + wd*w;  v = mu*v - lr*t;  w = w + v.
-__device__ __forceinline__ void update1(float &w, float &v, float g, float lr, float mu, float wd)
-{
-    const float t = __builtin_fmaf(wd, w, g);
-    v = __builtin_fmaf(mu, v, -(lr * t));
-    w = w + v;
-}
-
-template <bool ONCE> __device__ __forceinline__ f32x4 load4(const f32x4 *p)
-{
-    if constexpr (ONCE) return __builtin_nontemporal_load(p);
-    else return *p;
-}
-
+//
 // SNAP: 0 = update only, 1 = also write the new parameters to `copy` as fp32, 2 = as bf16 (round to nearest even):
 // the worker copy of the next fetch comes out of the same pass instead of a second read of the parameters.
-__device__ inline uint32_t f32_to_bf16_bits(uint32_t u);
 // The work of block `blk` of an update over n parameters whose buffers are 16-byte aligned (n4 = n / 4 whole vectors;
 // block 0 also takes the n % 4 elements behind them).
 template <int SNAP, bool ONCE>
@@ -114,11 +91,6 @@ __global__ __launch_bounds__(256) void update_kernel(f32x4 *__restrict__ w, f32x
 // the same pass (PushRanges): a block finds its range.  A range whose start is not a multiple of 4 elements runs element by
 // element.  Bound by memory.  62.4 M parameters: 204 us without a copy (the update 209, each fetch by a snapshot of its own 75 more); 2
 // bytes more a parameter and copy in bf16.
-__device__ __forceinline__ uint2 bf16x4(const f32x4 &v)
-{
-    return make_uint2(f32_to_bf16_bits(__float_as_uint(v.x)) | (f32_to_bf16_bits(__float_as_uint(v.y)) << 16),
-                      f32_to_bf16_bits(__float_as_uint(v.z)) | (f32_to_bf16_bits(__float_as_uint(v.w)) << 16));
-}
 __device__ __forceinline__ void push_one(const PushRanges &p, size_t i)
 {
     const float g = p.g[i];
@@ -360,11 +332,6 @@ int launch_accumulate(float *acc, const float *g, size_t n, bool first, hipStrea
 }
 
 // ---------------------------------------------------------------- snapshot
-__device__ inline uint32_t f32_to_bf16_bits(uint32_t u)  // round to nearest even; NaN -> quiet NaN
-{
-    if ((u & 0x7F800000u) == 0x7F800000u && (u & 0x007FFFFFu)) return (u >> 16) | 0x0040u;
-    return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
-}
 
 __global__ __launch_bounds__(256) void snapshot_kernel(const float *__restrict__ src, void *__restrict__ dst, size_t n, int to_bf16, int vec,
                                                        const int *version_counter, int32_t *log_slot, int log_update, int log_worker)

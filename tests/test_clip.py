@@ -1,0 +1,370 @@
+"""Norms over many tensors, clipping and clipped updates through the C ABI, against the formulas in 64 bits.
+
+Tolerances: squares are summed in 64 bits, so a norm is off by its rounding to fp32, half a step (2^-24).  A clipped element is the product of
+its value and a factor in 64 bits, rounded to fp32 and then to its type (half a step each)."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_1312_6186_amd import binding as B
+from paper_1312_6186_amd import workloads as wl
+
+DEV = "cuda:0"
+TDT = {B.F32: torch.float32, B.BF16: torch.bfloat16}
+vp = ctypes.c_void_p
+
+
+def _arr(*ptrs):
+    return (vp * len(ptrs))(*ptrs)
+
+
+def _cnt(*counts):
+    return (ctypes.c_size_t * len(counts))(*counts)
+
+
+# ---- without a GPU: refusals come before any work on it
+def test_norm_and_clip_refuse_bad_arguments():
+    L = B.lib()
+    ws, g, c, n = vp(1 << 20), _arr(1 << 12, 1 << 13), _arr(1 << 14, 1 << 15), _cnt(16, 16)
+    f = ctypes.c_float
+
+    def norm(grads=g, counts=n, k=2, dt=B.F32, out=vp(64), w=ws):
+        return L.asgd_grad_norm(grads, counts, k, dt, out, w, None)
+
+    def clip(grads=g, clipped=c, counts=n, k=2, dt=B.F32, m=1.0, out=vp(64), w=ws):
+        return L.asgd_clip_grads(grads, clipped, counts, k, dt, f(m), out, w, None)
+
+    for call in (norm, clip):
+        assert call(k=-1) == B.EINVAL
+        assert call(dt=7) == B.EINVAL and "dtype" in B.asgd_last_error()
+        assert call(grads=None) == B.EINVAL and call(counts=None) == B.EINVAL
+        assert call(grads=_arr(1 << 12, 0)) == B.EINVAL and "tensor 1" in B.asgd_last_error()
+        assert call(w=None) == B.EINVAL
+        assert call(w=vp((1 << 20) + 8)) == B.EALIGN
+        assert call(out=vp(66)) == B.EALIGN
+        assert call(grads=_arr(1 << 12, (1 << 13) + 2)) == B.EALIGN
+        assert call(grads=_arr(1 << 12, (1 << 13) + 1), dt=B.BF16) == B.EALIGN
+        assert call(counts=_cnt(16, 1 << 60)) == B.EINVAL
+    assert norm(out=None) == B.EINVAL
+    assert clip(clipped=None) == B.EINVAL and clip(clipped=_arr(1 << 14, 0)) == B.EINVAL
+    for bad in (0.0, -1.0, math.nan):
+        assert clip(m=bad) == B.EINVAL and "max_norm" in B.asgd_last_error()
+    assert B.asgd_grad_norm_workspace_bytes(1000) >= B.asgd_grad_norm_workspace_bytes(1) > 0
+
+
+def test_clip_refuses_overlapping_tensors():
+    L = B.lib()
+
+    def clip(grads, clipped, counts):
+        return L.asgd_clip_grads(_arr(*grads), _arr(*clipped), _cnt(*counts), len(grads), B.F32, ctypes.c_float(1.0), None, vp(1 << 20), None)
+
+    k = 4096
+    assert clip([k, k], [k, k], [8, 8]) == B.EINVAL                          # the same tensor twice, in place
+    assert clip([k, 2 * k], [3 * k, 3 * k + 28], [8, 8]) == B.EINVAL         # two clipped tensors share an element
+    assert clip([k, 2 * k], [2 * k, 3 * k], [8, 8]) == B.EINVAL              # the first is clipped into the second
+    assert clip([k, 2 * k], [k + 16, 3 * k], [8, 8]) == B.EINVAL             # shifted into itself
+    assert clip([3 * k, k, 2 * k], [5 * k, 6 * k, 3 * k - 4], [8, 8, 8]) == B.EINVAL
+    assert clip([k, k], [k, 3 * k], [8, 8]) == B.EINVAL                      # read for the second tensor, written by the first
+    assert "overlap" in B.asgd_last_error()
+
+
+def test_clipped_updates_refuse_bad_arguments():
+    L = B.lib()
+    f = ctypes.c_float
+
+    def call(w=16, v=16, g=16, n=10, m=1.0, copy=16, dt=B.F32, norm=16, ws=16):
+        return L.asgd_apply_update_clipped(vp(w), vp(v), vp(g), n, f(0.1), f(0.9), f(0.0), f(m), vp(copy), dt, vp(norm), vp(ws), None)
+
+    assert call(w=0) == B.EINVAL and call(v=0) == B.EINVAL and call(g=0) == B.EINVAL and call(ws=0) == B.EINVAL
+    assert call(dt=3) == B.EINVAL and call(m=0.0) == B.EINVAL and call(m=math.nan) == B.EINVAL
+    assert call(w=18) == B.EALIGN and call(copy=18) == B.EALIGN and call(copy=17, dt=B.BF16) == B.EALIGN and call(norm=18) == B.EALIGN and call(ws=24) == B.EALIGN
+    net = B.asgd_net_create(wl.TINY["layers"], 8, (1, 28, 28), B.F32)
+
+    def step(net_=net, w=16, m=1.0, ws=16, images=16):
+        return L.asgd_train_step_clipped(net_, vp(w), vp(16), vp(16), vp(images), vp(16), 0, 0, 0, vp(16), vp(16), f(0.1), f(0.9), f(0.0), f(m), vp(16),
+                                         vp(ws), None)
+
+    assert step(net_=None) == B.EINVAL and step(w=0) == B.EINVAL and step(m=-1.0) == B.EINVAL and step(ws=0) == B.EINVAL and step(images=0) == B.EINVAL
+    assert step(w=20) == B.EALIGN and step(ws=20) == B.EALIGN and step(images=20) == B.EALIGN
+    B.asgd_net_destroy(net)
+
+
+def test_lists_of_other_sizes_are_refused():
+    a, b = torch.zeros(8), torch.zeros(9)
+    with pytest.raises(ValueError):
+        B.asgd_clip_grads([a], [b], B.F32, 1.0, None, None)
+    with pytest.raises(ValueError):
+        B.asgd_clip_grads([a, a], [a], B.F32, 1.0, None, None)
+
+
+# ---- on the GPU
+def _workspace(n):
+    return torch.empty(B.asgd_grad_norm_workspace_bytes(n), dtype=torch.uint8, device=DEV).fill_(255)   # as NaN as it can be
+
+
+# lengths of tensors that lie one after the other in a vector, `gap` elements apart, from element `shift` on
+LAYOUTS = {"one": ([1], 0, 0), "short": ([3, 1, 0, 7, 2], 0, 0), "vector": ([4096], 0, 0), "tail": ([4099], 1, 0), "shifted": ([5000, 77, 1, 16385], 3, 1),
+           "tiles": ([16384 * 3 + 5, 0, 8191, 8192, 1], 0, 5), "many": ([1 + (37 * i) % 300 for i in range(300)], 1, 3), "long": ([3_000_001, 17, 900_000], 2, 1)}
+
+
+def _vector(layout, dtype, seed, scale=1.0):
+    sizes, shift, gap = LAYOUTS[layout]
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    total = shift + sum(sizes) + gap * len(sizes)
+    flat = (torch.randn(total, generator=gen, device=DEV) * scale).to(TDT[dtype])
+    views, at = [], shift
+    for s in sizes:
+        views.append(flat[at:at + s])
+        at += s + gap
+    return flat, views
+
+
+def _norm64(views):
+    return math.sqrt(sum(float((v.double() ** 2).sum()) for v in views))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("layout", list(LAYOUTS))
+def test_norm_over_tensors(layout, dtype):
+    flat, views = _vector(layout, dtype, 1)
+    norm = torch.full((1,), -1.0, device=DEV)
+    B.asgd_grad_norm(views, dtype, norm, _workspace(len(views)))
+    ref = _norm64(views)
+    assert abs(norm.item() - ref) <= (2.0 ** -24 + 2.0 ** -40) * ref
+    again = torch.full((1,), -1.0, device=DEV)
+    B.asgd_grad_norm(B.TensorList(views), dtype, again, _workspace(len(views)))
+    assert again.item() == norm.item()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [1e30, 1e-38])
+def test_norm_of_values_whose_squares_leave_the_range(scale):
+    flat, views = _vector("tiles", B.F32, 2, scale)
+    norm, ref = torch.empty(1, device=DEV), None
+    B.asgd_grad_norm(views, B.F32, norm, _workspace(len(views)))
+    ref = _norm64(views)
+    assert abs(norm.item() - ref) <= (2.0 ** -24 + 2.0 ** -40) * ref
+
+
+@pytest.mark.gpu
+def test_norm_of_nothing_and_of_a_tensor_twice():
+    norm = torch.full((1,), -1.0, device=DEV)
+    B.asgd_grad_norm([], B.F32, norm, _workspace(0))
+    assert norm.item() == 0.0
+    empty = torch.empty(0, device=DEV)
+    norm.fill_(-1.0)
+    B.asgd_clip_grads([empty, empty], [empty, empty], B.F32, 1.0, norm, _workspace(2))
+    assert norm.item() == 0.0
+    x = torch.full((9,), 2.0, device=DEV)
+    B.asgd_grad_norm([x, x], B.F32, norm, _workspace(2))
+    assert abs(norm.item() - math.sqrt(72.0)) <= 2.0 ** -24 * 9
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("place", ["apart", "shifted", "in place"])
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("layout", list(LAYOUTS))
+def test_clipped_tensors(layout, dtype, place):
+    flat, views = _vector(layout, dtype, 3)
+    ref_norm = _norm64(views)
+    max_norm = float(np.float32(0.37 * ref_norm))
+    before = flat.clone()
+    if place == "in place":
+        whole, outs = flat, views
+    else:
+        off = 1 if place == "shifted" else 0     # clipped tensors start elsewhere in their 16 bytes
+        whole = torch.full((flat.numel() + 8,), 7.0, dtype=flat.dtype, device=DEV)
+        start = flat.data_ptr()
+        es = flat.element_size()
+        outs = [whole[(v.data_ptr() - start) // es + off:][:v.numel()] if v.numel() else whole[:0] for v in views]
+    norm = torch.empty(1, device=DEV)
+    B.asgd_clip_grads(views, outs, dtype, max_norm, norm, _workspace(len(views)))
+    assert abs(norm.item() - ref_norm) <= (2.0 ** -24 + 2.0 ** -40) * ref_norm
+    mask = torch.ones_like(whole, dtype=torch.bool)
+    es, start = whole.element_size(), whole.data_ptr()
+    factor = max_norm / ref_norm
+    tol = torch.finfo(TDT[dtype]).eps / 2 * (1 + 2.0 ** -20) + 2.0 ** -22
+    for v, o in zip(views, outs):
+        if v.numel() == 0:
+            continue
+        src = before[(v.data_ptr() - flat.data_ptr()) // es:][:v.numel()]
+        ref = src.double() * factor
+        assert ((o.double() - ref).abs() <= tol * ref.abs()).all()
+        mask[(o.data_ptr() - start) // es:][:o.numel()] = False
+    # nothing else is written
+    assert torch.equal(whole[mask], (before if place == "in place" else torch.full_like(whole, 7.0))[mask])
+    if place != "in place":
+        assert torch.equal(flat, before)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+def test_a_gradient_within_the_norm_keeps_its_bits(dtype):
+    flat, views = _vector("shifted", dtype, 4)
+    before, out = flat.clone(), torch.zeros_like(flat)
+    n = _norm64(views)
+    for m in (1.01 * n, math.inf):
+        B.asgd_clip_grads(views, views, dtype, m, None, _workspace(len(views)))
+        assert torch.equal(flat, before)
+        es = flat.element_size()
+        outs = [out[(v.data_ptr() - flat.data_ptr()) // es:][:v.numel()] for v in views]
+        B.asgd_clip_grads(views, outs, dtype, m, None, _workspace(len(views)))
+        for v, o in zip(views, outs):
+            assert torch.equal(v, o)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("where", [0, 1, -1])
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+def test_a_gradient_that_is_not_finite_is_dropped(dtype, where, value):
+    flat, views = _vector("tail", dtype, 5)
+    views[0][where] = value
+    norm = torch.zeros(1, device=DEV)
+    out = torch.full_like(views[0], 3.0)
+    B.asgd_clip_grads(views, [out], dtype, math.inf, norm, _workspace(1))
+    assert (out == 0).all()
+    assert math.isnan(norm.item()) if math.isnan(value) else norm.item() == math.inf
+    B.asgd_clip_grads(views, views, dtype, 1.0, None, _workspace(1))
+    assert (views[0] == 0).all()
+
+
+@pytest.mark.gpu
+def test_a_finite_gradient_beyond_the_range_of_a_norm_is_clipped():
+    x = torch.full((1000,), 3e38, device=DEV)
+    norm, out = torch.zeros(1, device=DEV), torch.zeros_like(x)
+    B.asgd_clip_grads([x], [out], B.F32, 2.0, norm, _workspace(1))
+    assert norm.item() == math.inf
+    assert ((out.double() - 2.0 / math.sqrt(1000.0)).abs() <= 2.0 ** -22 * 2.0 / math.sqrt(1000.0)).all()
+
+
+def _update_inputs(n, seed, shift):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    w, v, g = (torch.randn(n + shift, generator=gen, device=DEV)[shift:] for _ in range(3))
+    return w, 0.1 * v if shift == 0 else v, g
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("copy", [None, B.F32, B.BF16])
+@pytest.mark.parametrize("share", [0.25, 2.0])
+@pytest.mark.parametrize("n,shift", [(1, 0), (3, 0), (4, 0), (1023, 0), (4096, 0), (1_000_003, 0), (5000, 1)])
+def test_clipped_update_is_clipping_then_updating(n, shift, share, copy):
+    lr, mu, wd = 0.05, 0.9, 1e-3
+    w, v, g = _update_inputs(n, 6, shift)
+    w2, v2, gc, g0 = w.clone(), v.clone(), torch.empty_like(g), g.clone()
+    m = share * float(g.double().norm())
+    norm, norm2 = torch.zeros(1, device=DEV), torch.zeros(1, device=DEV)
+    tdt = TDT[copy if copy is not None else B.F32]
+    c, c2 = torch.zeros(n, dtype=tdt, device=DEV), torch.zeros(n, dtype=tdt, device=DEV)
+    B.asgd_apply_update_clipped(w, v, g, lr, mu, wd, m, None if copy is None else c, B.F32 if copy is None else copy, norm, _workspace(1))
+    B.asgd_clip_grads([g], [gc], B.F32, m, norm2, _workspace(1))
+    if copy is None:
+        B.asgd_apply_update(w2, v2, gc, lr, mu, wd)
+    else:
+        B.asgd_apply_update_snapshot(w2, v2, gc, lr, mu, wd, c2, copy)
+    assert torch.equal(w, w2) and torch.equal(v, v2) and torch.equal(c, c2) and torch.equal(g, g0) and norm.item() == norm2.item()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [24_000_001, 62_000_003])    # within the memory-side cache, and beyond it
+def test_clipped_update_of_long_vectors(n):
+    lr, mu, wd, m = 0.05, 0.9, 1e-3, 100.0
+    w, v, g = _update_inputs(n, 7, 0)
+    c = torch.empty(n, dtype=torch.bfloat16, device=DEV)
+    w0, v0 = w.clone(), v.clone()
+    B.asgd_apply_update_clipped(w, v, g, lr, mu, wd, m, c, B.BF16, None, _workspace(1))
+    gc = torch.empty_like(g)
+    B.asgd_clip_grads([g], [gc], B.F32, m, None, _workspace(1))
+    B.asgd_apply_update(w0, v0, gc, lr, mu, wd)
+    assert torch.equal(w, w0) and torch.equal(v, v0) and torch.equal(c, w.to(torch.bfloat16))
+    f = m / float(g.double().norm())
+    assert ((gc.double() - g.double() * f).abs() <= 2.0 ** -22 * (g.double() * f).abs()).all()
+
+
+@pytest.mark.gpu
+def test_a_dropped_push_moves_parameters_by_momentum_alone():
+    w, v, g = _update_inputs(4097, 8, 0)
+    g[4096] = math.nan
+    w2, v2 = w.clone(), v.clone()
+    B.asgd_apply_update_clipped(w, v, g, 0.05, 0.9, 1e-3, 1.0, None, B.F32, None, _workspace(1))
+    B.asgd_apply_update(w2, v2, torch.zeros_like(g), 0.05, 0.9, 1e-3)
+    assert torch.equal(w, w2) and torch.equal(v, v2) and bool(torch.isfinite(w).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+def test_training_steps_with_clipped_pushes(dtype):
+    """Steps of the 32 x 32 net in one call against gradient, norm over the layers' slices, clipping and update in calls of their own."""
+    cfg = wl.SMALL
+    batch, tdt = 16, TDT[dtype]
+    net = B.asgd_net_create(cfg["layers"], batch, cfg["in_shape"], dtype)
+    try:
+        P = B.asgd_param_count(net)
+        w = torch.from_numpy(wl.make_params(cfg["layers"], cfg["in_shape"], 11)).to(DEV)
+        w2, v, v2 = w.clone(), torch.zeros(P, device=DEV), torch.zeros(P, device=DEV)
+        c, c2 = torch.empty(P, dtype=tdt, device=DEV), torch.empty(P, dtype=tdt, device=DEV)
+        g, g2, loss, loss2 = torch.empty(P, device=DEV), torch.empty(P, device=DEV), torch.empty(1, device=DEV), torch.empty(1, device=DEV)
+        norm, norm2 = torch.empty(1, device=DEV), torch.empty(1, device=DEV)
+        slices = [g2[o:o + n] for t in B.asgd_param_layout(net) for o, n in ((t["w_offset"], t["w_count"]), (t["b_offset"], t["b_count"]))]
+        assert sum(s.numel() for s in slices) == P
+        B.asgd_snapshot(w, c, dtype)
+        B.asgd_snapshot(w2, c2, dtype)
+        for step in range(3):
+            images, labels = wl.make_batch(cfg["in_shape"], batch, cfg["classes"], 20 + step)
+            img, lab = torch.from_numpy(images).to(DEV).to(tdt), torch.from_numpy(labels).to(DEV)
+            B.asgd_train_step_clipped(net, w, v, c, img, lab, 5, step, 0, loss, g, 0.01, 0.9, 5e-4, 0.5, norm, _workspace(1))
+            B.asgd_fwd_bwd(net, c2, img, lab, 5, step, 0, loss2, g2)
+            B.asgd_clip_grads(slices, slices, B.F32, 0.5, norm2, _workspace(len(slices)))
+            B.asgd_apply_update_snapshot(w2, v2, g2, 0.01, 0.9, 5e-4, c2, dtype)
+            assert norm.item() > 0.5 and loss.item() == loss2.item()
+            # one vector or its slices: the same squares in another order, in 64 bits; a factor a step apart moves a parameter by lr * 0.5 * 2^-22 at most
+            assert abs(norm.item() - norm2.item()) <= 2.0 ** -23 * norm.item()
+            assert torch.allclose(w, w2, rtol=2.0 ** -20, atol=2e-9) and torch.allclose(v, v2, rtol=2.0 ** -20, atol=2e-9)
+            w2.copy_(w); v2.copy_(v); c2.copy_(c)
+    finally:
+        torch.cuda.synchronize()
+        B.asgd_net_destroy(net)
+
+
+@pytest.mark.gpu
+def test_captured_calls_replay_and_streams_do_not_meet():
+    """One graph with a norm, a clipping and a clipped update, replayed between eager calls on another stream with a workspace of their own."""
+    flat, views = _vector("long", B.F32, 9)
+    out = torch.empty_like(flat)
+    es = flat.element_size()
+    outs = [out[(v.data_ptr() - flat.data_ptr()) // es:][:v.numel()] for v in views]
+    w, v, _ = _update_inputs(flat.numel(), 10, 0)
+    ws, ws2 = _workspace(len(views)), _workspace(len(views))
+    norm, norm2 = torch.zeros(2, device=DEV), torch.zeros(1, device=DEV)
+
+    def work(n, wsp):
+        B.asgd_clip_grads(views, outs, B.F32, 1.5, n[:1], wsp)
+        B.asgd_apply_update_clipped(w, v, flat, 0.01, 0.9, 0.0, 2.5, None, B.F32, n[1:], wsp)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work(norm, ws)
+    side = torch.cuda.Stream()
+    for k in range(4):
+        flat.mul_(1.25)
+        w0, v0 = w.clone(), v.clone()
+        torch.cuda.synchronize()
+        graph.replay()
+        with torch.cuda.stream(side):
+            B.asgd_grad_norm(views, B.F32, norm2, ws2)
+        torch.cuda.synchronize()
+        got, got_w, got_v = out.clone(), w.clone(), v.clone()
+        assert norm[0].item() == norm2.item()
+        w.copy_(w0); v.copy_(v0)
+        out.zero_()
+        n = torch.zeros(2, device=DEV)
+        work(n, ws2)
+        for o, s in zip(outs, views):
+            at = (o.data_ptr() - out.data_ptr()) // es
+            assert torch.equal(got[at:at + s.numel()], o)
+        assert torch.equal(got_w, w) and torch.equal(got_v, v) and torch.equal(n, norm)
