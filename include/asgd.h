@@ -378,6 +378,56 @@ int asgd_replay_nsync_run(asgd_net_t *const *nets, int n_workers, int n_sync, fl
  * Errors: ASGD_EINVAL (null with n > 0), ASGD_EALIGN, ASGD_EHIP. */
 int asgd_accumulate(float *accum, const float *grads, size_t n, int first, void *stream);
 
+/* ---- group normalisation ----------------------------------------------------
+ * Channel-last activations x: `batch` images of `pixels` pixels of `channels`
+ * channels; a pixel starts ldx elements behind the one before it, an image
+ * pixels * ldx elements behind the one before it.  Of every image, each of
+ * `groups` groups of neighbouring channels is normalised by itself, so that the
+ * result does not depend on the minibatch a replica happens to have:
+ *     mean, var over the group's channels and all pixels of the image
+ *     rstd = 1 / sqrt(var + eps),   h = (x - mean) * rstd
+ *     y = act(gamma[c] * h + beta[c])
+ *   x, y    : device, in `dtype` (ASGD_F32 or ASGD_BF16), aligned to their
+ *             elements (fastest where pointers, strides and channels are
+ *             multiples of 16 bytes).  y may be x (with ldy = ldx), or other
+ *             columns of the same rows; it must not overlap x in another way.
+ *             Columns behind the channels are neither read nor written.
+ *   gamma, beta : device, [channels] in `dtype`; null means 1 and 0.
+ *   mean, rstd  : device fp32 [batch][groups], what the backward pass needs;
+ *             null means not wanted.
+ *   act     : asgd_act_t.
+ *   workspace : device, asgd_group_norm_workspace_bytes(...) bytes, 16-byte
+ *             aligned; its contents do not matter, and calls that may overlap on
+ *             the GPU need one each.
+ * Sums are held in 32 bits within a thread and in 64 bits between them, in a
+ * fixed order.  An infinity or a NaN in x makes its group of its image NaN and
+ * no other.  With no images or no pixels nothing is written.
+ * Errors: ASGD_EINVAL (null, unknown dtype or act, eps not > 0 and finite,
+ * overlap), ASGD_ESHAPE (negative sizes, channels not a multiple of groups,
+ * strides below channels, more than 2^30 pixels or 2^31 groups in all),
+ * ASGD_EALIGN, ASGD_EHIP. */
+typedef enum {
+    ASGD_ACT_NONE = 0,
+    ASGD_ACT_RELU = 1,
+    ASGD_ACT_SILU = 2   /* z / (1 + exp(-z)) */
+} asgd_act_t;
+size_t asgd_group_norm_workspace_bytes(int batch, int pixels, int channels, int groups, int dtype);
+int asgd_group_norm_fwd(const void *x, const void *gamma, const void *beta, void *y, float *mean,
+                        float *rstd, int batch, int pixels, int channels, int groups, int64_t ldx,
+                        int64_t ldy, float eps, int act, int dtype, void *workspace, void *stream);
+/* Its gradients, with mean and rstd of the forward pass:
+ *   dy      : the gradient at y (pixels lddy apart); dx receives that at x (lddx).
+ *             dx may be dy or x (with the same stride).
+ *   dgamma, dbeta : device fp32 [channels], overwritten; null means not wanted.
+ * A ReLU lets the gradient through where gamma * h + beta > 0, decided without
+ * rounding for the given mean and rstd.  With no images or no pixels dgamma and
+ * dbeta are zero.
+ * Errors: as asgd_group_norm_fwd. */
+int asgd_group_norm_bwd(const void *dy, const void *x, const void *gamma, const void *beta,
+                        const float *mean, const float *rstd, void *dx, float *dgamma, float *dbeta,
+                        int batch, int pixels, int channels, int groups, int64_t lddy, int64_t ldx,
+                        int64_t lddx, int act, int dtype, void *workspace, void *stream);
+
 /* ---- gradients bounded by their norm --------------------------------------
  * A replica that is several updates old can push a gradient that is far too
  * large for the parameters it meets.  norm = sqrt(sum of g^2) over all elements

@@ -13,6 +13,7 @@ LIB_PATH = os.path.join(HERE, "libasgd_mi355x.so")
 
 F32, BF16 = 0, 1
 LAYER_CONV, LAYER_RELU, LAYER_MAXPOOL, LAYER_FC, LAYER_DROPOUT, LAYER_SOFTMAX_CE, LAYER_LRN = 1, 2, 3, 4, 5, 6, 7
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 DEBUG_OUTPUT, DEBUG_ARGMAX, DEBUG_MASK = 0, 1, 2
 OK, EINVAL, ESHAPE, ENOMEM, EHIP, EALIGN = 0, -1, -2, -3, -4, -5
 
@@ -22,7 +23,7 @@ EXPORTS = ["asgd_net_create", "asgd_net_prepare", "asgd_net_destroy", "asgd_net_
            "asgd_apply_update_snapshot", "asgd_train_step", "asgd_train_step_fused",
            "asgd_debug_get", "asgd_profile_begin", "asgd_profile_end", "asgd_schedule_generate", "asgd_replay_run", "asgd_replay_nsync_run", "asgd_accumulate", "asgd_apply_update_adagrad", "asgd_apply_update_adadelta",
            "asgd_grad_norm_workspace_bytes", "asgd_grad_norm", "asgd_clip_grads", "asgd_apply_update_clipped", "asgd_train_step_clipped",
-           "asgd_last_error"]
+           "asgd_group_norm_workspace_bytes", "asgd_group_norm_fwd", "asgd_group_norm_bwd", "asgd_last_error"]
 KERNEL_CLASSES = ["conv_fwd", "conv_dgrad", "conv_wgrad", "fc_fwd", "fc_dgrad", "fc_wgrad", "pool_fwd", "pool_bwd",
                   "bias_grad", "softmax_ce", "layout", "update", "lrn"]
 
@@ -103,6 +104,10 @@ def lib():
                                                 ctypes.c_int, vp, vp, vp]
         L.asgd_train_step_clipped.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.c_uint64, ctypes.c_uint64, ctypes.c_uint32, vp, vp, ctypes.c_float,
                                               ctypes.c_float, ctypes.c_float, ctypes.c_float, vp, vp, vp]
+        L.asgd_group_norm_workspace_bytes.argtypes = [ctypes.c_int] * 5
+        L.asgd_group_norm_workspace_bytes.restype = ctypes.c_size_t
+        L.asgd_group_norm_fwd.argtypes = [vp] * 6 + [ctypes.c_int] * 4 + [ctypes.c_int64] * 2 + [ctypes.c_float, ctypes.c_int, ctypes.c_int, vp, vp]
+        L.asgd_group_norm_bwd.argtypes = [vp] * 9 + [ctypes.c_int] * 4 + [ctypes.c_int64] * 3 + [ctypes.c_int, ctypes.c_int, vp, vp]
         L.asgd_last_error.restype = ctypes.c_char_p
         _lib = L
     return _lib
@@ -345,3 +350,18 @@ def asgd_train_step_clipped(net, master, momentum, worker_copy, images, labels, 
                             workspace, stream=None):
     _check(lib().asgd_train_step_clipped(net, _ptr(master), _ptr(momentum), _ptr(worker_copy), _ptr(images), _ptr(labels), dropout_seed, step, worker,
                                          _ptr(loss), _ptr(grads), lr, mu, wd, max_norm, _ptr(norm), _ptr(workspace), _stream(stream)))
+
+
+def asgd_group_norm_workspace_bytes(batch, pixels, channels, groups, dtype):
+    return int(lib().asgd_group_norm_workspace_bytes(batch, pixels, channels, groups, dtype))
+
+
+def asgd_group_norm_fwd(x, gamma, beta, y, mean, rstd, batch, pixels, channels, groups, ldx, ldy, eps, act, dtype, workspace, stream=None):
+    _check(lib().asgd_group_norm_fwd(_ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd), batch, pixels, channels, groups, ldx, ldy, eps,
+                                     act, dtype, _ptr(workspace), _stream(stream)))
+
+
+def asgd_group_norm_bwd(dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, batch, pixels, channels, groups, lddy, ldx, lddx, act, dtype, workspace,
+                        stream=None):
+    _check(lib().asgd_group_norm_bwd(_ptr(dy), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dgamma), _ptr(dbeta), batch, pixels,
+                                     channels, groups, lddy, ldx, lddx, act, dtype, _ptr(workspace), _stream(stream)))

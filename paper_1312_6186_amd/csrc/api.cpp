@@ -1795,4 +1795,78 @@ int asgd_train_step_clipped(asgd_net_t *net, float *master, float *momentum, voi
     return ASGD_OK;
 }
 
+// ---- group normalisation
+namespace {
+int check_group_norm(const char *name, const GroupNorm &q, uintptr_t tensors, uintptr_t params, uintptr_t stats, const void *workspace)
+{
+    if (q.dtype != ASGD_F32 && q.dtype != ASGD_BF16) return fail(ASGD_EINVAL, "%s: unknown dtype %d", name, q.dtype);
+    if (q.act != ASGD_ACT_NONE && q.act != ASGD_ACT_RELU && q.act != ASGD_ACT_SILU) return fail(ASGD_EINVAL, "%s: unknown activation %d", name, q.act);
+    if (q.batch < 0 || q.pixels < 0 || q.channels <= 0 || q.groups <= 0 || q.channels % q.groups)
+        return fail(ASGD_ESHAPE, "%s: %d images of %d pixels of %d channels in %d groups", name, q.batch, q.pixels, q.channels, q.groups);
+    if (q.ldx < q.channels || q.ldo < q.channels || q.lddy < q.channels) return fail(ASGD_ESHAPE, "%s: a pixel's stride is below its %d channels", name, q.channels);
+    const double pixels = (double)q.batch * q.pixels;
+    if (q.pixels > 1 << 30 || (double)q.batch * q.groups >= 2147483648.0 || pixels * (double)std::max(q.ldx, std::max(q.ldo, q.lddy)) > 1e15)
+        return fail(ASGD_ESHAPE, "%s: sizes too large", name);
+    const size_t es = dtype_size(q.dtype);
+    if (((tensors | params) & (es - 1)) || (stats & 3) || ((uintptr_t)workspace & 15)) return fail(ASGD_EALIGN, "%s: misaligned buffer", name);
+    return ASGD_OK;
+}
+
+// Whether an output tensor shares elements with an input tensor that it does not replace element by element.
+bool bad_overlap(const GroupNorm &q, const void *in, long ldi, const void *out)
+{
+    const long es = (long)dtype_size(q.dtype), rows = (long)q.batch * q.pixels;
+    if (in == out && ldi == q.ldo) return false;
+    const intptr_t a = (intptr_t)in, b = (intptr_t)out;
+    const intptr_t a_end = a + ((rows - 1) * ldi + q.channels) * es, b_end = b + ((rows - 1) * q.ldo + q.channels) * es;
+    if (a_end <= b || b_end <= a) return false;
+    if (ldi != q.ldo) return true;
+    const intptr_t pitch = ldi * es, r = ((b - a) % pitch + pitch) % pitch;   // other columns of the same rows
+    return r < q.channels * es || r > pitch - q.channels * es;
+}
+}  // namespace
+
+size_t asgd_group_norm_workspace_bytes(int batch, int pixels, int channels, int groups, int dtype)
+{
+    if (batch < 0 || pixels < 0 || channels <= 0 || groups <= 0 || (dtype != ASGD_F32 && dtype != ASGD_BF16)) return 0;
+    return group_norm_ws(batch, pixels, channels, groups, dtype);
+}
+
+int asgd_group_norm_fwd(const void *x, const void *gamma, const void *beta, void *y, float *mean, float *rstd, int batch, int pixels, int channels, int groups,
+                        int64_t ldx, int64_t ldy, float eps, int act, int dtype, void *workspace, void *stream)
+{
+    const GroupNorm q{dtype, act, batch, pixels, channels, groups, ldx, ldx, ldy};
+    const int rc = check_group_norm("asgd_group_norm_fwd", q, (uintptr_t)x | (uintptr_t)y, (uintptr_t)gamma | (uintptr_t)beta, (uintptr_t)mean | (uintptr_t)rstd,
+                                    workspace);
+    if (rc != ASGD_OK) return rc;
+    if (!(eps > 0.f && eps <= 3.4028234e38f)) return fail(ASGD_EINVAL, "asgd_group_norm_fwd: eps must be positive and finite");
+    if (batch == 0 || pixels == 0) return ASGD_OK;
+    if (!x || !y || !workspace) return fail(ASGD_EINVAL, "asgd_group_norm_fwd: null argument");
+    if (bad_overlap(q, x, ldx, y)) return fail(ASGD_EINVAL, "asgd_group_norm_fwd: y overlaps x");
+    if (launch_group_norm_fwd(q, x, gamma, beta, y, mean, rstd, eps, workspace, static_cast<hipStream_t>(stream)) != 0)
+        return hip_fail(hipGetLastError(), "group normalisation kernels");
+    return ASGD_OK;
+}
+
+int asgd_group_norm_bwd(const void *dy, const void *x, const void *gamma, const void *beta, const float *mean, const float *rstd, void *dx, float *dgamma,
+                        float *dbeta, int batch, int pixels, int channels, int groups, int64_t lddy, int64_t ldx, int64_t lddx, int act, int dtype,
+                        void *workspace, void *stream)
+{
+    const GroupNorm q{dtype, act, batch, pixels, channels, groups, ldx, lddy, lddx};
+    const int rc = check_group_norm("asgd_group_norm_bwd", q, (uintptr_t)dy | (uintptr_t)x | (uintptr_t)dx, (uintptr_t)gamma | (uintptr_t)beta,
+                                    (uintptr_t)mean | (uintptr_t)rstd | (uintptr_t)dgamma | (uintptr_t)dbeta, workspace);
+    if (rc != ASGD_OK) return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (batch == 0 || pixels == 0) {
+        if (dgamma && launch_fill_zero(dgamma, (size_t)channels * 4, st) != 0) return hip_fail(hipGetLastError(), "fill kernel");
+        if (dbeta && launch_fill_zero(dbeta, (size_t)channels * 4, st) != 0) return hip_fail(hipGetLastError(), "fill kernel");
+        return ASGD_OK;
+    }
+    if (!dy || !x || !mean || !rstd || !dx || !workspace) return fail(ASGD_EINVAL, "asgd_group_norm_bwd: null argument");
+    if (bad_overlap(q, dy, lddy, dx) || bad_overlap(q, x, ldx, dx)) return fail(ASGD_EINVAL, "asgd_group_norm_bwd: dx overlaps dy or x");
+    if (launch_group_norm_bwd(q, dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, workspace, st) != 0)
+        return hip_fail(hipGetLastError(), "group normalisation kernels");
+    return ASGD_OK;
+}
+
 }  // extern "C"

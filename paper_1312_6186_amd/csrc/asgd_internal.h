@@ -257,6 +257,18 @@ long pool_bwd_bands(int dtype, int B, int H, int W, int Cp, int k, int stride);
 int launch_lrn_fwd(int dtype, const void *a, void *y, size_t pixels, int Cp, int size, float alpha, float beta, float bias, hipStream_t s);
 int launch_lrn_bwd(int dtype, const void *a, const void *dy, int relu, void *da, size_t pixels, int Cp, int size, float alpha, float beta,
                    float bias, hipStream_t s);
+// Group normalisation with an activation on channel-last tensors (group_norm.hip): gamma, beta, mean, rstd, dgamma and dbeta may be null in the calls
+// where the public entry points say so.  batch, pixels > 0.
+enum Act { kActNone = 0, kActRelu = 1, kActSilu = 2 };
+struct GroupNorm {
+    int dtype, act, batch, pixels, channels, groups;
+    long ldx, lddy, ldo;     // elements from pixel to pixel: of x, of dy (backward), of y or dx
+};
+size_t group_norm_ws(int batch, int pixels, int channels, int groups, int dtype);   // bytes of workspace, for both directions
+int launch_group_norm_fwd(const GroupNorm &q, const void *x, const void *gamma, const void *beta, void *y, float *mean, float *rstd, float eps, void *ws,
+                          hipStream_t s);
+int launch_group_norm_bwd(const GroupNorm &q, const void *dy, const void *x, const void *gamma, const void *beta, const float *mean, const float *rstd, void *dx,
+                          float *dgamma, float *dbeta, void *ws, hipStream_t s);
 // Normalisation and a pool of window k, stride 2, on top of it in one pass each: forward a -> pooled y and positions; backward
 // writes da, times [a > 0], from the gradient dy at the pool's output, and leaves the column sums of da in
 // bands[Cp][lrn_pool_bands(...)].  lrn_pool_bands is 0 where the pair does not run this way: where the kernels do not
