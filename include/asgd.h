@@ -23,7 +23,7 @@
  *     the last error of the calling thread is at asgd_last_error().  Nothing
  *     aborts or throws across this boundary.
  *   - Canonical layouts: images [B,C,H,W]; the flat parameter vector holds, for
- *     every conv / fc layer in descriptor order, the weights then the bias;
+ *     every conv / group norm / fc layer in descriptor order, the weights then the bias;
  *     conv weights [cout][cin][k][k], fc weights [out][in] with
  *     in = c*H*W + h*W + w.  Gradients and momentum use the same order.
  */
@@ -50,12 +50,13 @@ typedef enum { ASGD_F32 = 0, ASGD_BF16 = 1 } asgd_dtype_t;
 
 typedef enum {
     ASGD_LAYER_CONV = 1,       /* out, k, stride, pad                          */
-    ASGD_LAYER_RELU = 2,       /* must follow a CONV or an FC                  */
+    ASGD_LAYER_RELU = 2,       /* must follow a CONV, a GROUP_NORM or an FC    */
     ASGD_LAYER_MAXPOOL = 3,    /* k, stride (unpadded, floor rule)             */
     ASGD_LAYER_FC = 4,         /* out                                          */
     ASGD_LAYER_DROPOUT = 5,    /* p, scale; must directly follow FC + RELU      */
     ASGD_LAYER_SOFTMAX_CE = 6, /* last layer; follows an FC                    */
-    ASGD_LAYER_LRN = 7         /* k (window, odd, <= 9), p (alpha), scale (beta), bias; must directly follow CONV + RELU */
+    ASGD_LAYER_LRN = 7,        /* k (window, odd, <= 9), p (alpha), scale (beta), bias; must directly follow CONV + RELU */
+    ASGD_LAYER_GROUP_NORM = 8  /* groups, p (eps); must directly follow a CONV that has no RELU of its own */
 } asgd_layer_kind_t;
 
 /* One entry of the network description.  Unused fields are ignored.
@@ -64,30 +65,34 @@ typedef enum {
  * cited unscaled form).
  * LRN is the cross-channel response normalisation of the architecture the paper
  * trains (Section 3 cites it):  b[c] = a[c] * (bias + alpha * sum a[c']^2)^(-beta),
- * the sum over the `k` channels centred on c, clipped at the ends. */
+ * the sum over the `k` channels centred on c, clipped at the ends.
+ * GROUP_NORM is asgd_group_norm_fwd over the convolution's output, with the RELU
+ * that follows it (if one does) as its activation; its gamma and beta, [channels]
+ * each, are parameters of the net like a layer's weights and bias. */
 typedef struct {
     int32_t kind;   /* asgd_layer_kind_t */
     int32_t out;    /* CONV: output channels; FC: output features */
     int32_t k;      /* CONV / MAXPOOL: square window size */
     int32_t stride; /* CONV / MAXPOOL */
     int32_t pad;    /* CONV: zero padding on each side */
-    float p;        /* DROPOUT: drop probability, 0 <= p < 1; LRN: alpha */
+    float p;        /* DROPOUT: drop probability, 0 <= p < 1; LRN: alpha; GROUP_NORM: eps (0 is read as 1e-5) */
     float scale;    /* DROPOUT: factor on kept units; LRN: beta */
     float bias;     /* LRN: the additive constant k of the formula */
     int32_t groups; /* CONV: number of channel groups ("columns"); 0 or 1 = ungrouped.  Group g maps input
                        channels [g*cin/groups, ...) to output channels [g*out/groups, ...); both per-group
-                       counts must be multiples of 8; filters are [out][cin/groups][k][k] */
+                       counts must be multiples of 8; filters are [out][cin/groups][k][k].
+                       GROUP_NORM: number of groups, a divisor of the channels */
 } asgd_layer_desc_t;
 
 /* Where one parameterised layer lives in the flat parameter vector. */
 typedef struct {
     int32_t layer;       /* index into the descriptor list */
-    int32_t kind;        /* ASGD_LAYER_CONV or ASGD_LAYER_FC */
+    int32_t kind;        /* ASGD_LAYER_CONV, ASGD_LAYER_FC or ASGD_LAYER_GROUP_NORM (weights: gamma, bias: beta) */
     uint64_t w_offset;   /* elements from the start of the flat vector */
     uint64_t w_count;
     uint64_t b_offset;
     uint64_t b_count;
-    int32_t w_shape[4];  /* conv: cout,cin,k,k; fc: out,in,1,1 */
+    int32_t w_shape[4];  /* conv: cout,cin,k,k; fc: out,in,1,1; group norm: channels,1,1,1 */
 } asgd_tensor_info_t;
 
 typedef struct asgd_net asgd_net_t;
@@ -295,7 +300,9 @@ typedef enum {
     ASGD_K_CONV_FWD = 0, ASGD_K_CONV_DGRAD = 1, ASGD_K_CONV_WGRAD = 2,
     ASGD_K_FC_FWD = 3, ASGD_K_FC_DGRAD = 4, ASGD_K_FC_WGRAD = 5,
     ASGD_K_POOL_FWD = 6, ASGD_K_POOL_BWD = 7, ASGD_K_BIAS_GRAD = 8,
-    ASGD_K_SOFTMAX_CE = 9, ASGD_K_LAYOUT = 10, ASGD_K_UPDATE = 11, ASGD_K_LRN = 12, ASGD_K_COUNT = 13
+    ASGD_K_SOFTMAX_CE = 9, ASGD_K_LAYOUT = 10, ASGD_K_UPDATE = 11,
+    ASGD_K_LRN = 12,   /* both normalisations */
+    ASGD_K_COUNT = 13
 } asgd_kernel_class_t;
 typedef struct {
     int32_t kclass;

@@ -2,9 +2,10 @@
 
 A network is a list of layer tuples:
     ("conv", cout, k, stride, pad)  ("relu",)  ("maxpool", k, stride)
-    ("fc", out)  ("dropout", p[, scale])  ("softmax_ce",)
+    ("fc", out)  ("dropout", p[, scale])  ("softmax_ce",)  ("groupnorm", groups[, eps])
 The flat parameter vector holds, for each conv/fc layer in order, the weights
-(conv [cout,cin,k,k]; fc [out,in] with in = c*H*W + h*W + w) followed by the bias.
+(conv [cout,cin,k,k]; fc [out,in] with in = c*H*W + h*W + w) followed by the bias
+(group normalisation: the scale of every channel, then the shift).
 Section 2 of the paper defines the unit of work: the gradient of the objective
 over one minibatch.
 """
@@ -46,6 +47,11 @@ class OracleNet:
                 self.param_slices[li] = (off, wshape, off + l[1] * nin, l[1])
                 off += l[1] * nin + l[1]
                 shape = (l[1],)
+            elif kind == "groupnorm":
+                c = shape[0]
+                assert len(shape) == 3 and c % l[1] == 0
+                self.param_slices[li] = (off, (c,), off + c, c)
+                off += 2 * c
             elif kind in ("relu", "dropout", "softmax_ce", "lrn"):
                 pass
             else:
@@ -113,6 +119,9 @@ class OracleNet:
                     x, t["argmax"] = ops.maxpool_fwd(x, l[1], l[2])
             elif kind == "lrn":   # ("lrn", size, alpha, beta, k)
                 x = ops.lrn_fwd(x, l[1], l[2], l[3], l[4])
+            elif kind == "groupnorm":
+                w, b = self.split(params, li)
+                x, t["h"], t["rstd"] = ops.group_norm_fwd(x, w, b, l[1], l[2] if len(l) > 2 else 1e-5)
             elif kind == "fc":
                 w, b = self.split(params, li)
                 x = ops.fc_fwd(x.reshape(N, -1), w, b)
@@ -130,7 +139,7 @@ class OracleNet:
                 t["dz"] = dz
             if act_dtype == "bf16" and kind != "softmax_ce":
                 nxt = self.layers[li + 1][0]
-                stored = ((kind in ("conv", "fc") and nxt not in ("relu", "softmax_ce"))
+                stored = ((kind in ("conv", "fc", "groupnorm") and nxt not in ("relu", "softmax_ce"))
                           or (kind == "relu" and nxt != "dropout") or kind in ("dropout", "lrn"))
                 if stored:
                     x = ops.round_bf16(x)
@@ -163,6 +172,10 @@ class OracleNet:
                                     l[1], l[2])
             elif kind == "lrn":
                 d = ops.lrn_bwd(xin, d.reshape(xin.shape), l[1], l[2], l[3], l[4])
+            elif kind == "groupnorm":
+                w, b = self.split(params, li)
+                w_off, _, b_off, c = self.param_slices[li]
+                d, grads[w_off:w_off + c], grads[b_off:b_off + c] = ops.group_norm_bwd(d.reshape(xin.shape), trace[li]["h"], trace[li]["rstd"], w, l[1])
             elif kind == "fc":
                 w, b = self.split(params, li)
                 w_off, w_shape, b_off, b_len = self.param_slices[li]

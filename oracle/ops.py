@@ -189,6 +189,27 @@ def dropout_mask(count, seed, step, worker, layer, p):
     return mask
 
 
+def group_norm_fwd(x, gamma, beta, groups, eps):
+    """(y, h, rstd): x [N,C,H,W] normalised over each image's groups of channels, h = (x - mean) * rstd, y = gamma h + beta."""
+    x = _f64(x)
+    N, C = x.shape[:2]
+    v = x.reshape(N, groups, -1)
+    d = v - v.mean(axis=2, keepdims=True)
+    rstd = 1.0 / np.sqrt((d * d).mean(axis=2, keepdims=True) + eps)
+    h = (d * rstd).reshape(x.shape)
+    return h * gamma.reshape(1, C, 1, 1) + beta.reshape(1, C, 1, 1), h, rstd
+
+
+def group_norm_bwd(dy, h, rstd, gamma, groups):
+    """(dx, dgamma, dbeta)."""
+    dy = _f64(dy)
+    N, C = dy.shape[:2]
+    dh = (dy * gamma.reshape(1, C, 1, 1)).reshape(N, groups, -1)
+    hg = h.reshape(N, groups, -1)
+    dx = rstd * (dh - dh.mean(axis=2, keepdims=True) - hg * (dh * hg).mean(axis=2, keepdims=True))
+    return dx.reshape(dy.shape), (dy * h).sum(axis=(0, 2, 3)), dy.sum(axis=(0, 2, 3))
+
+
 def dropout_apply(r, mask, scale=1.0):
     r = _f64(r)
     mask = np.ascontiguousarray(mask, dtype=np.uint8)

@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libasgd_mi355x.so")
 
 F32, BF16 = 0, 1
-LAYER_CONV, LAYER_RELU, LAYER_MAXPOOL, LAYER_FC, LAYER_DROPOUT, LAYER_SOFTMAX_CE, LAYER_LRN = 1, 2, 3, 4, 5, 6, 7
+LAYER_CONV, LAYER_RELU, LAYER_MAXPOOL, LAYER_FC, LAYER_DROPOUT, LAYER_SOFTMAX_CE, LAYER_LRN, LAYER_GROUP_NORM = 1, 2, 3, 4, 5, 6, 7, 8
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 DEBUG_OUTPUT, DEBUG_ARGMAX, DEBUG_MASK = 0, 1, 2
 OK, EINVAL, ESHAPE, ENOMEM, EHIP, EALIGN = 0, -1, -2, -3, -4, -5
@@ -153,6 +153,8 @@ def layer_descs(layers):
             arr[i] = LayerDesc(LAYER_SOFTMAX_CE, 0, 0, 0, 0, 0.0, 0.0)
         elif kind == "lrn":    # ("lrn", size, alpha, beta, k)
             arr[i] = LayerDesc(LAYER_LRN, 0, l[1], 0, 0, float(l[2]), float(l[3]), float(l[4]))
+        elif kind == "groupnorm":    # ("groupnorm", groups[, eps])
+            arr[i] = LayerDesc(LAYER_GROUP_NORM, 0, 0, 0, 0, float(l[2]) if len(l) > 2 else 0.0, 0.0, 0.0, l[1])
         else:
             raise ValueError("unknown layer kind %r" % (kind,))
     return arr

@@ -38,7 +38,7 @@ int hip_fail(hipError_t e, const char *what) { return fail(ASGD_EHIP, "%s: %s", 
 
 inline int round_up(int v, int m) { return (v + m - 1) / m * m; }
 
-enum StageKind { ST_CONV = 1, ST_POOL = 2, ST_FC = 3, ST_LRN = 4 };
+enum StageKind { ST_CONV = 1, ST_POOL = 2, ST_FC = 3, ST_LRN = 4, ST_NORM = 5 };
 
 struct Stage {
     int kind = 0;
@@ -51,7 +51,8 @@ struct Stage {
     bool in_is_spatial = false;  // an fc fed by a conv / pool stage (flatten boundary)
     bool last = false;           // produces the fp32 logits
     int k = 0, stride = 1, pad = 0;
-    int groups = 1;   // convolution channel groups
+    int groups = 1;   // convolution channel groups; ST_NORM: groups that are normalised
+    float eps = 0.f;  // ST_NORM (relu: its activation)
     // window-row form (first stage, <= 4 input channels): bordered input [B][rwHp][rwWp][rwC], K = k * rwKW
     int rw = 0, rwC = 0, rwKW = 0, rwHp = 0, rwWp = 0;
     int relu = 0, drop = 0, drop_layer = -1;
@@ -59,7 +60,7 @@ struct Stage {
     float lrn_alpha = 0.f, lrn_beta = 0.f, lrn_bias = 0.f;   // ST_LRN (window size in k)
     bool to_flat = false;      // ST_POOL: writes the flattened input of the fully-connected layer above (and has no tensors of its own)
     bool with_pool = false;    // ST_LRN: one kernel does it together with the pool that follows (out is written for export only)
-    bool has_params() const { return kind == ST_CONV || kind == ST_FC; }
+    bool has_params() const { return kind == ST_CONV || kind == ST_FC || kind == ST_NORM; }
     float drop_p = 0.f, drop_scale = 1.f;
     uint32_t drop_thr = 0;
     size_t w_off = 0, w_cnt = 0, b_off = 0, b_cnt = 0;
@@ -75,6 +76,7 @@ struct Stage {
     WgradPlan d_wgrad;           // CONV: set where the filter gradient (of all groups) runs as conv_wgrad
     DirectPlan d_fwd, d_dgrad;   // CONV: set where the forward pass / the data gradient (of all groups) runs as conv_direct
     size_t wf_elems = 0, wd_elems = 0;   // packed filters of one group
+    float *mean = nullptr, *rstd = nullptr;   // ST_NORM, [images][groups]: from the forward pass to the backward pass
     size_t out_elems() const { return kind == ST_FC ? (size_t)out_ld : (size_t)outH * outW * outCp; }
 };
 
@@ -109,6 +111,8 @@ struct asgd_net {
     hipEvent_t replay_start = nullptr, replay_done = nullptr;
     hipEvent_t ev_join = nullptr, ev_bias = nullptr;
     std::vector<hipEvent_t> ev_dy, ev_dg;   // per stage: output gradient ready, data gradient issued
+    void *norm_ws = nullptr;          // of the group normalisations, which run one after the other
+    size_t norm_ws_bytes = 0;
     float *row_loss = nullptr;
     int *version_counter = nullptr;  // device-side count of applied updates (A-SGD replay)
     size_t scratch_floats = 0, scratch_side_floats = 0;
@@ -165,12 +169,17 @@ size_t carve(asgd_net &n, char *base)
         if (s.kind == ST_CONV) {
             s.wd = i > 0 ? at(s.wd_elems * s.groups * es) : nullptr;
         }
-        if (s.has_params()) s.colsum_ws = static_cast<float *>(at(s.colsum_floats * 4));
+        if (s.kind == ST_NORM) {
+            s.mean = static_cast<float *>(at(B * s.groups * 4));
+            s.rstd = static_cast<float *>(at(B * s.groups * 4));
+        }
+        if (s.kind == ST_CONV || s.kind == ST_FC) s.colsum_ws = static_cast<float *>(at(s.colsum_floats * 4));
         if (s.kind == ST_FC && s.in_is_spatial) {
             s.flat_in = at(B * s.in_f * es);
             s.dflat_in = at(B * s.in_f * es);
         }
     }
+    if (n.norm_ws_bytes) n.norm_ws = at(n.norm_ws_bytes);
     n.row_loss = static_cast<float *>(at(B * 4));
     n.version_counter = static_cast<int *>(at(256));
     n.scratch = static_cast<float *>(at(n.scratch_floats * 4));
@@ -276,6 +285,21 @@ int plan_net(asgd_net &n)
             s.inC = s.outC = C; s.inCp = s.outCp = round_up(C, 8); s.inH = s.outH = H; s.inW = s.outW = W;
             s.k = l.k; s.nonneg = true; s.lrn_alpha = l.p; s.lrn_beta = l.scale; s.lrn_bias = l.bias;
             n.layer_shape[3 * i] = C; n.layer_shape[3 * i + 1] = H; n.layer_shape[3 * i + 2] = W;
+        } else if (l.kind == ASGD_LAYER_GROUP_NORM) {
+            if (n.stages.empty() || n.stages.back().kind != ST_CONV || n.stages.back().relu)
+                return fail(ASGD_ESHAPE, "layer %d: GROUP_NORM must directly follow a CONV", i);
+            if (l.groups <= 0 || C % l.groups) return fail(ASGD_ESHAPE, "layer %d: GROUP_NORM of %d channels in %d groups", i, C, l.groups);
+            if (!(l.p >= 0.f && l.p <= 3.4028234e38f)) return fail(ASGD_ESHAPE, "layer %d: GROUP_NORM needs a finite eps >= 0", i);
+            s.kind = ST_NORM;
+            s.inC = s.outC = C; s.inCp = s.outCp = round_up(C, 8); s.inH = s.outH = H; s.inW = s.outW = W;
+            s.groups = l.groups; s.eps = l.p == 0.f ? 1e-5f : l.p;
+            s.w_off = off; s.w_cnt = C; s.b_off = off + C; s.b_cnt = C;
+            off += 2 * (size_t)C;
+            n.layer_shape[3 * i] = C; n.layer_shape[3 * i + 1] = H; n.layer_shape[3 * i + 2] = W;
+            if (i + 1 < L && n.layers[i + 1].kind == ASGD_LAYER_RELU) {
+                s.relu = 1; s.nonneg = true; ++i;
+                n.layer_shape[3 * i] = C; n.layer_shape[3 * i + 1] = H; n.layer_shape[3 * i + 2] = W;
+            }
         } else if (l.kind == ASGD_LAYER_FC) {
             if (l.out <= 0) return fail(ASGD_ESHAPE, "layer %d: bad FC size", i);
             s.kind = ST_FC;
@@ -313,7 +337,7 @@ int plan_net(asgd_net &n)
             ++i;
             break;
         } else if (l.kind == ASGD_LAYER_RELU) {
-            return fail(ASGD_ESHAPE, "layer %d: RELU must directly follow a CONV or an FC", i);
+            return fail(ASGD_ESHAPE, "layer %d: RELU must directly follow a CONV, a GROUP_NORM or an FC", i);
         } else if (l.kind == ASGD_LAYER_DROPOUT) {
             return fail(ASGD_ESHAPE, "layer %d: DROPOUT must directly follow FC + RELU", i);
         } else {
@@ -321,12 +345,13 @@ int plan_net(asgd_net &n)
         }
         s.last_layer = i;
         for (int j = s.first_layer; j <= s.last_layer; ++j) n.layer_stage[j] = (int)n.stages.size();
-        if ((s.kind == ST_CONV || s.kind == ST_FC)) {
+        if (s.has_params()) {
             asgd_tensor_info_t t;
             memset(&t, 0, sizeof t);
-            t.layer = s.first_layer; t.kind = s.kind == ST_CONV ? ASGD_LAYER_CONV : ASGD_LAYER_FC;
+            t.layer = s.first_layer; t.kind = n.layers[s.first_layer].kind;
             t.w_offset = s.w_off; t.w_count = s.w_cnt; t.b_offset = s.b_off; t.b_count = s.b_cnt;
-            if (s.kind == ST_CONV) { t.w_shape[0] = s.outC; t.w_shape[1] = s.inC / s.groups; t.w_shape[2] = s.k; t.w_shape[3] = s.k; }
+            if (s.kind == ST_NORM) { t.w_shape[0] = s.outC; t.w_shape[1] = t.w_shape[2] = t.w_shape[3] = 1; }
+            else if (s.kind == ST_CONV) { t.w_shape[0] = s.outC; t.w_shape[1] = s.inC / s.groups; t.w_shape[2] = s.k; t.w_shape[3] = s.k; }
             else { t.w_shape[0] = s.out_f; t.w_shape[1] = s.in_f; t.w_shape[2] = 1; t.w_shape[3] = 1; }
             n.tensors.push_back(t);
         }
@@ -390,7 +415,7 @@ int plan_net(asgd_net &n)
 int size_net(asgd_net &n, const Budget &partials, bool plain)
 {
     const long B = n.batch;
-    size_t scratch = 0, scratch_side = 0;
+    size_t scratch = 0, scratch_side = 0, norm_ws = 0;
     for (size_t si = 0; si < n.stages.size(); ++si) {
         Stage &s = n.stages[si];
         if (s.kind == ST_CONV) {
@@ -440,6 +465,8 @@ int size_net(asgd_net &n, const Budget &partials, bool plain)
                 n.stages[si + 1].with_pool = s.pool_bands > 0;
                 s.colsum_floats = std::max(s.colsum_floats, (size_t)s.pool_bands * s.outCp);
             }
+        } else if (s.kind == ST_NORM) {
+            norm_ws = std::max(norm_ws, group_norm_ws(n.batch, s.outH * s.outW, s.outC, s.groups, n.dtype));
         } else if (s.kind == ST_FC) {
             s.p_fwd = plan_gemm(B, s.out_ld, s.in_f, n.dtype, 32);
             s.p_dgrad = plan_gemm(B, s.in_f, s.out_f, n.dtype, 32);
@@ -448,6 +475,7 @@ int size_net(asgd_net &n, const Budget &partials, bool plain)
             s.colsum_floats = colsum_ws_floats(n.dtype, B, s.out_ld);
         }
     }
+    n.norm_ws_bytes = norm_ws;
     n.scratch_floats = scratch + kScratchSpare;
     n.scratch_side_floats = scratch_side + kScratchSpare;
     n.ws_bytes = carve(n, nullptr);
@@ -599,6 +627,12 @@ GemmPlan fc_plan(const asgd_net *n, GemmPlan p)
 
 const char *param_ptr(const asgd_net *n, const void *params, size_t off) { return static_cast<const char *>(params) + off * dtype_size(n->dtype); }
 
+// A group normalisation of the net.  Columns behind the channels stay the zeros that the workspace was cleared to.
+GroupNorm norm_args(const asgd_net *n, const Stage &s)
+{
+    return GroupNorm{n->dtype, s.relu ? kActRelu : kActNone, n->batch, s.outH * s.outW, s.outC, s.groups, s.outCp, s.outCp, s.outCp};
+}
+
 int forward(asgd_net *n, const void *params, const void *images, const int32_t *labels, uint64_t seed, uint64_t step, uint32_t worker, hipStream_t st)
 {
     const int B = n->batch, dt = n->dtype;
@@ -675,6 +709,11 @@ int forward(asgd_net *n, const void *params, const void *images, const int32_t *
         } else if (s.kind == ST_LRN) {
             ProfScope ps(n, st, ASGD_K_LRN, 0, 2 * Bd * s.outC * s.outH * s.outW * es);
             CHECK_LAUNCH(launch_lrn_fwd(dt, cur, s.out, (size_t)B * s.outH * s.outW, s.outCp, s.k, s.lrn_alpha, s.lrn_beta, s.lrn_bias, st), "lrn forward");
+        } else if (s.kind == ST_NORM) {
+            ProfScope ps(n, st, ASGD_K_LRN, 0, 2 * Bd * s.outC * s.outH * s.outW * es);
+            CHECK_LAUNCH(launch_group_norm_fwd(norm_args(n, s), cur, param_ptr(n, params, s.w_off), param_ptr(n, params, s.b_off), s.out, s.mean, s.rstd, s.eps,
+                                               n->norm_ws, st),
+                         "group normalisation forward");
         } else if (s.kind == ST_POOL) {
             ProfScope ps(n, st, ASGD_K_POOL_FWD, 0, Bd * s.outC * ((double)s.inH * s.inW * es + (double)s.outH * s.outW * (es + 1)));
             CHECK_LAUNCH(launch_pool_fwd(dt, cur, s.nonneg, s.out, s.argmax, B, s.inH, s.inW, s.inCp, s.k, s.stride, st), "pool forward");
@@ -903,7 +942,7 @@ int backward(asgd_net *n, const void *params, float *loss, float *grads, hipStre
         Stage &s = n->stages[si];
         Stage *prev = si > 0 ? &n->stages[si - 1] : nullptr;
         const void *xin = prev ? prev->out : n->act0;
-        if (fork && s.has_params()) {  // the gradient at this stage's output is complete on the caller's stream
+        if (fork && (s.kind == ST_CONV || s.kind == ST_FC)) {  // the gradient at this stage's output is complete on the caller's stream
             CHECK_HIP(hipEventRecord(n->ev_dy[si], st), "hipEventRecord");
             CHECK_HIP(hipStreamWaitEvent(sd, n->ev_dy[si], 0), "hipStreamWaitEvent");
         }
@@ -986,6 +1025,12 @@ int backward(asgd_net *n, const void *params, float *loss, float *grads, hipStre
             CHECK_LAUNCH(launch_lrn_bwd(dt, prev->out, s.dout, 1, prev->dout, (size_t)B * s.outH * s.outW, s.outCp, s.k, s.lrn_alpha, s.lrn_beta,
                                         s.lrn_bias, st),
                          "lrn backward");
+        } else if (s.kind == ST_NORM) {
+            // its parameters' gradients come with that of its input: on the caller's stream
+            ProfScope ps(n, st, ASGD_K_LRN, 0, 3 * Bd * s.outC * s.outH * s.outW * es);
+            CHECK_LAUNCH(launch_group_norm_bwd(norm_args(n, s), s.dout, prev->out, param_ptr(n, params, s.w_off), param_ptr(n, params, s.b_off), s.mean, s.rstd,
+                                               prev->dout, grads + s.w_off, grads + s.b_off, n->norm_ws, st),
+                         "group normalisation backward");
         } else if (s.kind == ST_POOL) {
             // prev exists: a pool cannot be first... unless the net starts with a pool, which feeds no parameters
             // a ReLU below has been applied to s.dout already by a CONV or FC above (relu_under_pool); only a pool

@@ -9,6 +9,7 @@ labels stand in for the ILSVRC-2012 data the paper trains on (Section 1).
 A network is a list of layer tuples:
     ("conv", cout, k, stride, pad[, groups])  ("relu",)  ("maxpool", k, stride)
     ("fc", out)  ("dropout", p)  ("softmax_ce",)  ("lrn", size, alpha, beta, k)
+    ("groupnorm", groups[, eps])
 """
 import numpy as np
 
@@ -59,11 +60,15 @@ ALEXNET_FULL = dict(ALEXNET, name="alexnet_full",
                             + _conv_block(384, 3, 1, 1) + _conv_block(384, 3, 1, 1, groups=2)
                             + _conv_block(256, 3, 1, 1, (3, 2), groups=2) + ALEXNET["layers"][13:]))
 
-CONFIGS = {"tiny": TINY, "small": SMALL, "alexnet": ALEXNET, "alexnet_lrn": ALEXNET_LRN, "alexnet_full": ALEXNET_FULL}
+# the three-layer net with group normalisation between each convolution and its ReLU, for replicas with small minibatches
+SMALL_GN = dict(SMALL, name="small_gn",
+                layers=[y for x in SMALL["layers"] for y in ((x, ("groupnorm", 8)) if x[0] == "conv" else (x,))])
+
+CONFIGS = {"tiny": TINY, "small": SMALL, "alexnet": ALEXNET, "alexnet_lrn": ALEXNET_LRN, "alexnet_full": ALEXNET_FULL, "small_gn": SMALL_GN}
 
 
 def param_shapes(layers, in_shape):
-    """[(layer index, weight shape, bias length, fan_in)] in flat-buffer order."""
+    """[(layer index, weight shape, bias length, fan_in)] in flat-buffer order; fan_in 0: a normalisation's scale and shift."""
     shape = tuple(in_shape)
     out = []
     for li, l in enumerate(layers):
@@ -77,6 +82,8 @@ def param_shapes(layers, in_shape):
             _, k, s = l
             c, h, w = shape
             shape = (c, (h - k) // s + 1, (w - k) // s + 1)
+        elif l[0] == "groupnorm":
+            out.append((li, (shape[0],), shape[0], 0))
         elif l[0] == "fc":
             nin = int(np.prod(shape))
             out.append((li, (l[1], nin), l[1], nin))
@@ -89,12 +96,15 @@ def param_count(layers, in_shape):
 
 
 def make_params(layers, in_shape, seed):
-    """He-normal weights N(0, 2/fan_in), zero biases, as one flat fp32 vector."""
+    """He-normal weights N(0, 2/fan_in), zero biases, scales of one, as one flat fp32 vector."""
     rng = np.random.default_rng(seed)
     parts = []
     for _, wshape, blen, fan_in in param_shapes(layers, in_shape):
         n = int(np.prod(wshape))
-        parts.append((rng.standard_normal(n, dtype=np.float32) * np.float32(np.sqrt(2.0 / fan_in))))
+        if fan_in == 0:
+            parts.append(np.ones(n, dtype=np.float32))
+        else:
+            parts.append((rng.standard_normal(n, dtype=np.float32) * np.float32(np.sqrt(2.0 / fan_in))))
         parts.append(np.zeros(blen, dtype=np.float32))
     return np.concatenate(parts)
 
