@@ -17,6 +17,8 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
+#include <numeric>
 
 #include "asgd_internal.h"
 #include "stream.h"
@@ -29,6 +31,17 @@ constexpr int kThreads = 256, kUnroll = 4;
 
 // V values of type T as they lie in memory.
 template <typename T, int V> struct alignas(sizeof(T) * V) Pack { T e[V]; };
+
+// What the compiler knows of a pack's values ends here: packs are widened anew by the next pass over them instead of being kept in 32 bits, which would
+// take twice the registers.
+template <typename T, int V> __device__ __forceinline__ void forget(Pack<T, V> &p)
+{
+    uint32_t w[sizeof(p) / 4];
+    __builtin_memcpy(w, &p, sizeof(p));
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(p) / 4; ++i) asm volatile("" : "+v"(w[i]));
+    __builtin_memcpy(&p, w, sizeof(p));
+}
 
 template <int ACT> __device__ __forceinline__ float activate(float z)
 {
@@ -43,34 +56,40 @@ __device__ __forceinline__ float silu_slope(float z)
     return s * __builtin_fmaf(z, 1.f - s, 1.f);
 }
 
-__device__ __forceinline__ float round_down(double t)
+// The next fp32 value below f, and the largest one that is not above t.
+__device__ __forceinline__ float below(float f)
 {
-    const float f = (float)t;
-    if (!((double)f > t)) return f;
     const uint32_t u = __float_as_uint(f);
     return __uint_as_float(f > 0.f ? u - 1 : f < 0.f ? u + 1 : 0x80000001u);
 }
+__device__ __forceinline__ float round_down(double t)
+{
+    const float f = (float)t;
+    return (double)f > t ? below(f) : f;
+}
 
-// What the backward pass knows of one channel of one image.
+// What the backward pass knows of one channel of one image, beside the mean of its group: z = (x - mean) * a + beta.
 template <int ACT> struct Channel {
-    float mean, a, beta;    // z = (x - mean) * a + beta
-    float sign, edge;       // ReLU: z > 0 is sign * x > edge
-    __device__ __forceinline__ void set(float m, float rstd, float gamma, float b)
+    float a, beta;     // ReLU: beta is the edge; z > 0 is x > edge where gamma > 0, and not x > edge (with the edge below t) where gamma < 0
+    bool falls;
+    __device__ __forceinline__ void set(float mean, float rstd, float gamma, float b)
     {
-        mean = m; a = rstd * gamma; beta = b; sign = edge = 0.f;
+        a = rstd * gamma; beta = b; falls = false;
         if constexpr (ACT == kActRelu) {
             if (gamma == 0.f) {
-                edge = b > 0.f ? -1.f : 1.f;
+                beta = b > 0.f ? -__builtin_inff() : __builtin_inff();
             } else {
-                sign = gamma > 0.f ? 1.f : -1.f;
-                edge = round_down((double)sign * ((double)m - (double)b / ((double)rstd * (double)gamma)));
+                const double t = (double)mean - (double)b / ((double)rstd * (double)gamma);
+                falls = gamma < 0.f;
+                beta = round_down(t);
+                if (falls && (double)beta == t) beta = below(beta);
             }
         }
     }
-    __device__ __forceinline__ float slope(float dy, float x) const   // dz
+    __device__ __forceinline__ float slope(float dy, float x, float d) const   // dz, with d = x - mean
     {
-        if constexpr (ACT == kActRelu) return sign * x > edge ? dy : 0.f;
-        if constexpr (ACT == kActSilu) return dy * silu_slope(__builtin_fmaf(x - mean, a, beta));
+        if constexpr (ACT == kActRelu) return (x > beta) != falls ? dy : 0.f;
+        if constexpr (ACT == kActSilu) return dy * silu_slope(__builtin_fmaf(d, a, beta));
         return dy;
     }
 };
@@ -188,6 +207,13 @@ __device__ __forceinline__ void wave_sum(double &a, double &b)
     for (int d = 32; d; d >>= 1) { a += __shfl_xor(a, d); b += __shfl_xor(b, d); }
 }
 
+// Mean and rstd from sum x and sum x^2 of M values.
+__device__ __forceinline__ float2 group_stats(double a, double b, double M, float eps)
+{
+    const double m = a / M, var = b / M - m * m;
+    return make_float2((float)m, (float)(1.0 / __builtin_sqrt((var > 0 ? var : var == var ? 0.0 : var) + (double)eps)));
+}
+
 // One wave per image and group: its mean and rstd.
 __global__ __launch_bounds__(kThreads) void gn_fwd_stats_kernel(GnShape s, const double *part, float eps, float *mean, float *rstd)
 {
@@ -204,9 +230,9 @@ __global__ __launch_bounds__(kThreads) void gn_fwd_stats_kernel(GnShape s, const
     }
     wave_sum(a, b);
     if ((threadIdx.x & 63) == 0) {
-        const double M = (double)s.P * s.cg, m = a / M, var = b / M - m * m;
-        mean[i] = (float)m;
-        rstd[i] = (float)(1.0 / __builtin_sqrt((var > 0 ? var : var == var ? 0.0 : var) + (double)eps));
+        const float2 st = group_stats(a, b, (double)s.P * s.cg, eps);
+        mean[i] = st.x;
+        rstd[i] = st.y;
     }
 }
 
@@ -244,13 +270,13 @@ __global__ __launch_bounds__(kThreads) void gn_fwd_apply_kernel(GnShape s, const
 
 template <typename T, int V, int ACT>
 __device__ __forceinline__ void load_channels(const GnShape &s, const Place &w, const T *gamma, const T *beta, const float *mean, const float *rstd,
-                                              Channel<ACT> (&ch)[V], float (&r)[V])
+                                              Channel<ACT> (&ch)[V], float (&m)[V], float (&r)[V])
 {
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         const int c = w.c0 + e, i = w.n * s.G + c / s.cg;
-        r[e] = rstd[i];
-        ch[e].set(mean[i], r[e], gamma ? ldf(&gamma[c]) : 1.f, beta ? ldf(&beta[c]) : 0.f);
+        m[e] = mean[i]; r[e] = rstd[i];
+        ch[e].set(m[e], r[e], gamma ? ldf(&gamma[c]) : 1.f, beta ? ldf(&beta[c]) : 0.f);
     }
 }
 
@@ -265,8 +291,8 @@ __global__ __launch_bounds__(kThreads) void gn_bwd_sums_kernel(GnShape s, const 
     for (int e = 0; e < V; ++e) sa[e] = sb[e] = 0.f;
     if (w.live) {
         Channel<ACT> ch[V];
-        float r[V];
-        load_channels<T, V, ACT>(s, w, gamma, beta, mean, rstd, ch, r);
+        float m[V], r[V];
+        load_channels<T, V, ACT>(s, w, gamma, beta, mean, rstd, ch, m, r);
         const size_t at = (size_t)w.n * s.P + w.p0 + w.row;
         const T *px = x + at * s.ldx + w.c0, *pd = dy + at * s.lddy + w.c0;
         const size_t xstep = (size_t)s.rows * s.ldx, dstep = (size_t)s.rows * s.lddy;
@@ -280,9 +306,9 @@ __global__ __launch_bounds__(kThreads) void gn_bwd_sums_kernel(GnShape s, const 
                 if (p + k * (long)s.rows >= w.p1) continue;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float xv = ldf(&vx[k].e[e]), dz = ch[e].slope(ldf(&vd[k].e[e]), xv);
+                    const float xv = ldf(&vx[k].e[e]), d = xv - m[e], dz = ch[e].slope(ldf(&vd[k].e[e]), xv, d);
                     sa[e] += dz;
-                    sb[e] = __builtin_fmaf(dz, xv - ch[e].mean, sb[e]);
+                    sb[e] = __builtin_fmaf(dz, d, sb[e]);
                 }
             }
         }
@@ -292,37 +318,15 @@ __global__ __launch_bounds__(kThreads) void gn_bwd_sums_kernel(GnShape s, const 
     channel_sums<V>(s, w, sa, sb, part, [](double2 &t, float2 v, int) ASGD_INLINE { t.x += (double)v.x; t.y += (double)v.y; });
 }
 
-// The first workgroups: one wave per image and group, (sum gamma A) / M and (sum gamma B) / M into coef.  The others: dgamma and dbeta of four
-// channels, 64 threads each over images and chunks.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void gn_bwd_stats_kernel(GnShape s, const double *part, const T *gamma, float2 *coef, float *dgamma, float *dbeta,
-                                                                unsigned group_blocks)
+// dgamma and dbeta of four channels, 64 threads each over `entries` (images and chunks of them).
+__device__ __forceinline__ void param_grads(const double *part, long entries, int C, int first, float *dgamma, float *dbeta)
 {
     __shared__ double2 lds[kThreads];
-    if (blockIdx.x < group_blocks) {
-        const unsigned i = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-        if (i >= (unsigned)s.N * (unsigned)s.G) return;
-        const unsigned n = i / s.G, g = i - n * s.G;
-        const double *p = part + ((size_t)n * s.chunks * s.C + (size_t)g * s.cg) * 2;
-        double a = 0, b = 0;
-        const long entries = (long)s.chunks * s.cg;
-        for (long j = threadIdx.x & 63; j < entries; j += 64) {
-            const long k = j / s.cg, c = j - k * s.cg;
-            const double *q = p + ((size_t)k * s.C + c) * 2;
-            const double w = gamma ? (double)ldf(&gamma[g * s.cg + c]) : 1.0;
-            a = __builtin_fma(w, q[0], a); b = __builtin_fma(w, q[1], b);
-        }
-        wave_sum(a, b);
-        const double M = (double)s.P * s.cg;
-        if ((threadIdx.x & 63) == 0) coef[i] = make_float2((float)(a / M), (float)(b / M));
-        return;
-    }
-    const int c = (int)(blockIdx.x - group_blocks) * 4 + ((int)threadIdx.x & 3);
+    const int c = first + ((int)threadIdx.x & 3);
     double2 t = make_double2(0, 0);
-    if (c < s.C) {
-        const long entries = (long)s.N * s.chunks;
+    if (c < C) {
         for (long j = threadIdx.x >> 2; j < entries; j += kThreads / 4) {
-            const double2 v = *reinterpret_cast<const double2 *>(part + ((size_t)j * s.C + c) * 2);
+            const double2 v = *reinterpret_cast<const double2 *>(part + ((size_t)j * C + c) * 2);
             t.x += v.x; t.y += v.y;
         }
     }
@@ -332,10 +336,40 @@ __global__ __launch_bounds__(kThreads) void gn_bwd_stats_kernel(GnShape s, const
         if ((int)threadIdx.x < d) { lds[threadIdx.x].x += lds[threadIdx.x + d].x; lds[threadIdx.x].y += lds[threadIdx.x + d].y; }
         __syncthreads();
     }
-    if (threadIdx.x < 4 && c < s.C) {
+    if (threadIdx.x < 4 && c < C) {
         if (dbeta) dbeta[c] = (float)lds[threadIdx.x].x;
         if (dgamma) dgamma[c] = (float)lds[threadIdx.x].y;
     }
+}
+__global__ __launch_bounds__(kThreads) void gn_param_grads_kernel(const double *part, long entries, int C, float *dgamma, float *dbeta)
+{
+    param_grads(part, entries, C, (int)blockIdx.x * 4, dgamma, dbeta);
+}
+
+// The first workgroups: one wave per image and group, (sum gamma A) / M and (sum gamma B) / M into coef.  The others: the parameters' gradients.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void gn_bwd_stats_kernel(GnShape s, const double *part, const T *gamma, float2 *coef, float *dgamma, float *dbeta,
+                                                                unsigned group_blocks)
+{
+    if (blockIdx.x >= group_blocks) {
+        param_grads(part, (long)s.N * s.chunks, s.C, (int)(blockIdx.x - group_blocks) * 4, dgamma, dbeta);
+        return;
+    }
+    const unsigned i = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    if (i >= (unsigned)s.N * (unsigned)s.G) return;
+    const unsigned n = i / s.G, g = i - n * s.G;
+    const double *p = part + ((size_t)n * s.chunks * s.C + (size_t)g * s.cg) * 2;
+    double a = 0, b = 0;
+    const long entries = (long)s.chunks * s.cg;
+    for (long j = threadIdx.x & 63; j < entries; j += 64) {
+        const long k = j / s.cg, c = j - k * s.cg;
+        const double *q = p + ((size_t)k * s.C + c) * 2;
+        const double w = gamma ? (double)ldf(&gamma[g * s.cg + c]) : 1.0;
+        a = __builtin_fma(w, q[0], a); b = __builtin_fma(w, q[1], b);
+    }
+    wave_sum(a, b);
+    const double M = (double)s.P * s.cg;
+    if ((threadIdx.x & 63) == 0) coef[i] = make_float2((float)(a / M), (float)(b / M));
 }
 
 template <typename T, int V, int ACT>
@@ -345,8 +379,8 @@ __global__ __launch_bounds__(kThreads) void gn_bwd_apply_kernel(GnShape s, const
     const Place w = place<V>(s);
     if (!w.live) return;
     Channel<ACT> ch[V];
-    float c0[V], c2[V];   // dx = a * dz - c0 - c2 * (x - mean)
-    load_channels<T, V, ACT>(s, w, gamma, beta, mean, rstd, ch, c2);
+    float m[V], c0[V], c2[V];   // dx = a * dz - c0 - c2 * (x - mean)
+    load_channels<T, V, ACT>(s, w, gamma, beta, mean, rstd, ch, m, c2);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         const float2 k = coef[w.n * s.G + (w.c0 + e) / s.cg];
@@ -367,12 +401,281 @@ __global__ __launch_bounds__(kThreads) void gn_bwd_apply_kernel(GnShape s, const
             if (p + k * (long)s.rows >= w.p1) continue;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float xv = ldf(&vx[k].e[e]), dz = ch[e].slope(ldf(&vd[k].e[e]), xv);
-                stf(&vd[k].e[e], __builtin_fmaf(-c2[e], xv - ch[e].mean, __builtin_fmaf(ch[e].a, dz, -c0[e])));
+                const float xv = ldf(&vx[k].e[e]), d = xv - m[e], dz = ch[e].slope(ldf(&vd[k].e[e]), xv, d);
+                stf(&vd[k].e[e], __builtin_fmaf(-c2[e], d, __builtin_fmaf(ch[e].a, dz, -c0[e])));
             }
             *reinterpret_cast<Pack<T, V> *>(po + k * ostep) = vd[k];
         }
     }
+}
+
+// ---- slabs: what a workgroup can hold of an image
+//
+// A workgroup takes whole groups of one image, all pixels, into registers: one read, one write, the sums between them in LDS.  Vectors do not
+// leave their workgroup's groups; with UNI they do not leave a group either, and what belongs to a group is held once.
+struct GnSlab {
+    int N, P, C, G, cg;
+    int width, blocks;       // channels of a workgroup (whole groups, whole vectors), workgroups per image
+    int bx, rows, full;      // vectors of a row, pixels at a time, turns in which all rows lie in the image
+    unsigned total;          // workgroups with work
+    int per;                 // of an XCD
+    long ldx, lddy, ldo;
+    FastDiv dblocks, dbx;
+};
+
+// Workgroups are dealt to the XCDs in turn; here each XCD gets a run of them, so that those that share the lines of an image's pixels share an L2.
+__device__ __forceinline__ unsigned slab_of(const GnSlab &s) { return (blockIdx.x & 7) * (unsigned)s.per + (blockIdx.x >> 3); }
+
+template <typename T, int V> __device__ __forceinline__ Pack<T, V> buf_pack(__amdgpu_buffer_rsrc_t rs, unsigned off)
+{
+    Pack<T, V> r;
+    if constexpr (sizeof(r) == 16) {
+        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, 0, 0);
+        __builtin_memcpy(&r, &v, 16);
+    } else {
+        static_assert(sizeof(r) == 8, "packs of 8 or 16 bytes");
+        const auto v = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)off, 0, 0);
+        __builtin_memcpy(&r, &v, 8);
+    }
+    return r;
+}
+template <typename T, int V> __device__ __forceinline__ void buf_store_pack(__amdgpu_buffer_rsrc_t rs, unsigned off, const Pack<T, V> &r)
+{
+    if constexpr (sizeof(r) == 16) {
+        u32x4 v;
+        __builtin_memcpy(&v, &r, 16);
+        __builtin_amdgcn_raw_buffer_store_b128(v, rs, (int)off, 0, 0);
+    } else {
+        typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+        u32x2 v;
+        __builtin_memcpy(&v, &r, 8);
+        __builtin_amdgcn_raw_buffer_store_b64(v, rs, (int)off, 0, 0);
+    }
+}
+// Image n of a tensor as a range of bytes, from the workgroup's first channel on: loads behind it give zeros, stores behind it are dropped.
+template <typename T> __device__ __forceinline__ __amdgpu_buffer_rsrc_t image(const GnSlab &s, const T *p, long ld, unsigned n, int c_first)
+{
+    const T *base = p + (size_t)n * s.P * ld + c_first;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(base), 0, (int)(((s.P - 1) * ld + s.C - c_first) * (long)sizeof(T)), 0x00020000);
+}
+constexpr unsigned kNowhere = 0x80000000u;   // images are shorter (checked on the host)
+
+// How many of the rows r, r + rows, ... lie in the image.
+__device__ __forceinline__ int pixels_of(const GnSlab &s, int r) { return s.full + (s.full * s.rows + r < s.P ? 1 : 0); }
+
+constexpr int kSlabThreads = 1024;
+
+template <typename T, int V, bool UNI, int R>
+__global__ __launch_bounds__(kSlabThreads) void gn_fwd_slab_kernel(GnSlab s, const T *x, const T *gamma, const T *beta, T *y, float *mean_out, float *rstd_out,
+                                                                   float eps, int act)
+{
+    constexpr int S = UNI ? 1 : V;     // statistics of a thread
+    extern __shared__ __align__(16) char shared[];
+    float2 *lds = reinterpret_cast<float2 *>(shared);                                             // [rows][bx][S]
+    double2 *sums = reinterpret_cast<double2 *>(shared + (size_t)blockDim.x * S * sizeof(float2));   // [wave]: of a group, or part of one
+    const unsigned L = slab_of(s);
+    if (L >= s.total) return;
+    const unsigned n = fdiv(L, s.dblocks), cb = L - n * s.blocks;
+    const int c_first = (int)cb * s.width, width = min(s.width, s.C - c_first), groups = width / s.cg;
+    const int row = (int)fdiv(threadIdx.x, s.dbx), vec = (int)threadIdx.x - row * s.bx;
+    const bool live = row < s.rows && vec * V < width;
+    const auto rx = image(s, x, s.ldx, n, c_first);
+    const unsigned step = (unsigned)(s.rows * s.ldx * (long)sizeof(T));
+    const unsigned at = live ? (unsigned)((row * s.ldx + vec * V) * (long)sizeof(T)) : kNowhere;
+    Pack<T, V> v[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) v[k] = buf_pack<T, V>(rx, live && k * s.rows + row < s.P ? at + k * step : kNowhere);
+    float ga[V], be[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        const int c = c_first + vec * V + e;
+        ga[e] = gamma && live ? ldf(&gamma[c]) : 1.f;
+        be[e] = beta && live ? ldf(&beta[c]) : 0.f;
+    }
+    // of the thread's values (its channels together, or each): their mean, and the squares about it, by way of its first one
+    const int count = live ? pixels_of(s, row) : 0;
+    float m[S], m2[S], pivot[S];
+#pragma unroll
+    for (int e = 0; e < S; ++e) { m[e] = m2[e] = 0.f; pivot[e] = ldf(&v[0].e[e]); }
+    static_for<0, R>([&](auto k) ASGD_INLINE {
+        if (k < count) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = ldf(&v[k].e[e]) - pivot[UNI ? 0 : e];
+                m[UNI ? 0 : e] += d;
+                m2[UNI ? 0 : e] = __builtin_fmaf(d, d, m2[UNI ? 0 : e]);
+            }
+        }
+    });
+    const float inv = count ? 1.f / (float)(count * (UNI ? V : 1)) : 0.f;
+#pragma unroll
+    for (int e = 0; e < S; ++e) {
+        const float d = m[e] * inv;
+        m2[e] = __builtin_fmaf(-m[e], d, m2[e]);
+        m[e] = pivot[e] + d;
+    }
+    if (row < s.rows) {
+#pragma unroll
+        for (int e = 0; e < S; ++e) lds[(row * s.bx + vec) * S + e] = make_float2(m[e], m2[e]);
+    }
+    __syncthreads();
+    // Waves share out the groups, or parts of their rows: sum x and sum x^2 in 64 bits
+    const int waves = (int)blockDim.x / 64, wave = (int)threadIdx.x / 64, lane = (int)threadIdx.x & 63;
+    const int parts = max(1, waves / groups), used = min(s.rows, s.P), gs = s.cg / (UNI ? V : 1);   // entries of a row of a group
+    for (int base = 0; base < groups; base += waves) {
+        const int part = groups < waves ? wave / groups : 0, g = groups < waves ? wave - part * groups : base + wave;
+        double a = 0, b = 0;
+        if (part < parts && g < groups) {
+            for (int r = part; r < used; r += parts) {
+                const double cnt = (double)(pixels_of(s, r) * (UNI ? V : 1));
+                for (int q = lane; q < gs; q += 64) {
+                    const float2 p = lds[(r * s.bx) * S + g * gs + q];
+                    const double cm = cnt * (double)p.x;
+                    a += cm;
+                    b += __builtin_fma(cm, (double)p.x, (double)p.y);
+                }
+            }
+        }
+        wave_sum(a, b);
+        if (lane == 0 && part < parts && g < groups) sums[part * groups + g] = make_double2(a, b);
+    }
+    __syncthreads();
+    float2 *stat = lds;   // free now
+    if ((int)threadIdx.x < groups) {
+        double a = 0, b = 0;
+        for (int p = 0; p < parts; ++p) { a += sums[p * groups + threadIdx.x].x; b += sums[p * groups + threadIdx.x].y; }
+        const float2 st = group_stats(a, b, (double)s.P * s.cg, eps);
+        stat[threadIdx.x] = st;
+        const size_t i = (size_t)n * s.G + c_first / s.cg + threadIdx.x;
+        if (mean_out) mean_out[i] = st.x;
+        if (rstd_out) rstd_out[i] = st.y;
+    }
+    __syncthreads();
+    if (!live) return;
+    float mean[S];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        const float2 st = stat[(vec * V + e) / s.cg];
+        if (e < S) mean[e] = st.x;
+        ga[e] *= st.y;
+    }
+    const auto ry = image(s, y, s.ldo, n, c_first);
+    const unsigned ostep = (unsigned)(s.rows * s.ldo * (long)sizeof(T)), oat = (unsigned)((row * s.ldo + vec * V) * (long)sizeof(T));
+    const auto store = [&](auto a) ASGD_INLINE {
+        static_for<0, R>([&](auto k) ASGD_INLINE {
+            if (k >= count) return;
+            forget(v[k]);
+#pragma unroll
+            for (int e = 0; e < V; ++e) stf(&v[k].e[e], activate<decltype(a)::value>(__builtin_fmaf(ldf(&v[k].e[e]) - mean[UNI ? 0 : e], ga[e], be[e])));
+            buf_store_pack<T, V>(ry, oat + k * ostep, v[k]);
+        });
+    };
+    if (act == kActRelu) store(std::integral_constant<int, kActRelu>{});
+    else if (act == kActSilu) store(std::integral_constant<int, kActSilu>{});
+    else store(std::integral_constant<int, kActNone>{});
+}
+
+// A and B of each image and channel go to part, for the parameters' gradients.
+template <typename T, int V, bool UNI, int R, int ACT>
+__global__ __launch_bounds__(kSlabThreads) void gn_bwd_slab_kernel(GnSlab s, const T *dy, const T *x, const T *gamma, const T *beta, const float *mean,
+                                                                   const float *rstd, T *dx, double *part_out)
+{
+    constexpr int S = UNI ? 1 : V;
+    extern __shared__ __align__(16) char shared[];
+    float2 *lds = reinterpret_cast<float2 *>(shared);                                                // [rows][bx * V]
+    double2 *sums = reinterpret_cast<double2 *>(shared + (size_t)blockDim.x * V * sizeof(float2));   // [thread]
+    const unsigned L = slab_of(s);
+    if (L >= s.total) return;
+    const unsigned n = fdiv(L, s.dblocks), cb = L - n * s.blocks;
+    const int c_first = (int)cb * s.width, width = min(s.width, s.C - c_first), groups = width / s.cg;
+    const int row = (int)fdiv(threadIdx.x, s.dbx), vec = (int)threadIdx.x - row * s.bx;
+    const bool live = row < s.rows && vec * V < width;
+    const auto rx = image(s, x, s.ldx, n, c_first), rd = image(s, dy, s.lddy, n, c_first);
+    const unsigned xstep = (unsigned)(s.rows * s.ldx * (long)sizeof(T)), dstep = (unsigned)(s.rows * s.lddy * (long)sizeof(T));
+    const unsigned xat = (unsigned)((row * s.ldx + vec * V) * (long)sizeof(T)), dat = (unsigned)((row * s.lddy + vec * V) * (long)sizeof(T));
+    const int count = live ? pixels_of(s, row) : 0;
+    Pack<T, V> vx[R], vd[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        vx[k] = buf_pack<T, V>(rx, k < count ? xat + k * xstep : kNowhere);
+        vd[k] = buf_pack<T, V>(rd, k < count ? dat + k * dstep : kNowhere);
+    }
+    Channel<ACT> ch[V];
+    float m[S], r[S];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        const int c = live ? c_first + vec * V + e : 0;
+        const size_t i = (size_t)n * s.G + c / s.cg;
+        const float me = mean[i], re = rstd[i];
+        if (e < S) { m[e] = me; r[e] = re; }
+        ch[e].set(me, re, gamma ? ldf(&gamma[c]) : 1.f, beta ? ldf(&beta[c]) : 0.f);
+    }
+    float sa[V], sb[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) sa[e] = sb[e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {   // zeros of dy behind the image add nothing
+            const float xv = ldf(&vx[k].e[e]), d = xv - m[UNI ? 0 : e], dz = ch[e].slope(ldf(&vd[k].e[e]), xv, d);
+            sa[e] += dz;
+            sb[e] = __builtin_fmaf(dz, d, sb[e]);
+        }
+    }
+    if (row < s.rows) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) lds[row * s.bx * V + vec * V + e] = make_float2(sa[e], sb[e] * r[UNI ? 0 : e]);
+    }
+    __syncthreads();
+    // threads share out the channels, or parts of their rows
+    const int pitch = s.bx * V, threads = (int)blockDim.x, parts = threads / pitch, used = min(s.rows, s.P);
+    {
+        const int part = (int)threadIdx.x / pitch, c = (int)threadIdx.x - part * pitch;
+        double2 t = make_double2(0, 0);
+        if (part < parts) {
+            for (int q = part; q < used; q += parts) { const float2 p = lds[q * pitch + c]; t.x += (double)p.x; t.y += (double)p.y; }
+            sums[threadIdx.x] = t;
+        }
+    }
+    __syncthreads();
+    if (const int c = (int)threadIdx.x; c < width) {
+        double2 t = sums[c];
+        for (int p = 1; p < parts; ++p) { t.x += sums[p * pitch + c].x; t.y += sums[p * pitch + c].y; }
+        reinterpret_cast<double2 *>(part_out)[(size_t)n * s.C + c_first + c] = t;
+        const double g = gamma ? (double)ldf(&gamma[c_first + c]) : 1.0;
+        sums[c] = make_double2(g * t.x, g * t.y);
+    }
+    __syncthreads();
+    float2 *coef = lds;
+    const int wave = (int)threadIdx.x / 64, lane = (int)threadIdx.x & 63;
+    for (int g = wave; g < groups; g += threads / 64) {
+        double a = 0, b = 0;
+        for (int c = lane; c < s.cg; c += 64) { a += sums[g * s.cg + c].x; b += sums[g * s.cg + c].y; }
+        wave_sum(a, b);
+        if (lane == 0) coef[g] = make_float2((float)(a / ((double)s.P * s.cg)), (float)(b / ((double)s.P * s.cg)));
+    }
+    __syncthreads();
+    if (!live) return;
+    float c0[S], c2[S];   // dx = a * dz - c0 - c2 * (x - mean)
+#pragma unroll
+    for (int e = 0; e < S; ++e) {
+        const float2 k = coef[(vec * V + e) / s.cg];
+        c0[e] = r[e] * k.x;
+        c2[e] = r[e] * r[e] * k.y;
+    }
+    const auto ro = image(s, dx, s.ldo, n, c_first);
+    const unsigned ostep = (unsigned)(s.rows * s.ldo * (long)sizeof(T)), oat = (unsigned)((row * s.ldo + vec * V) * (long)sizeof(T));
+    static_for<0, R>([&](auto k) ASGD_INLINE {
+        if (k >= count) return;
+        forget(vx[k]);
+        forget(vd[k]);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float xv = ldf(&vx[k].e[e]), d = xv - m[UNI ? 0 : e], dz = ch[e].slope(ldf(&vd[k].e[e]), xv, d);
+            stf(&vd[k].e[e], __builtin_fmaf(-c2[UNI ? 0 : e], d, __builtin_fmaf(ch[e].a, dz, -c0[UNI ? 0 : e])));
+        }
+        buf_store_pack<T, V>(ro, oat + k * ostep, vd[k]);
+    });
 }
 
 // ---- host side
@@ -413,6 +716,83 @@ bool gn_shape(const GroupNorm &q, int V, GnShape &s)
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
+// ---- slabs, host side
+
+// VGPRs that a thread's part of one tensor may take
+constexpr int kFwdRegs[] = {8, 16, 32, 72}, kBwdRegs[] = {8, 16, 36};
+
+// What a choice costs, for comparison alone.
+double slab_cost(int piece, int threads, int regs, double total, double bytes)
+{
+    // lines of 128 bytes that a piece of a pixel touches, over what it uses of them; rounds over the CUs
+    const double lines = (piece + 127) / 128 * 128.0 / piece;
+    const int fit = std::max(1, std::min(2048 / threads, (regs <= 16 ? 2048 : 1024) / threads));
+    const double rounds = std::ceil(total / (256.0 * fit));
+    return rounds * fit * bytes * lines;
+}
+
+struct SlabPlan { int V = 0, uni = 0, threads = 0, regs = 0; GnSlab s; };
+
+// The slabs of a call; V = 0 where there are none: vectors below 8 bytes, images that do not fit, strides beyond 32-bit offsets.
+template <int N> SlabPlan plan_slab(const GroupNorm &q, int V, const int (&regs)[N])
+{
+    SlabPlan best;
+    const int es = (int)dtype_size(q.dtype), cg = q.channels / q.groups;
+    if (cg % V && V * es == 16 && es == 2) V /= 2;     // per-channel statistics for four channels at most
+    if (V * es < 8) return best;
+    const long ld = std::max(q.ldx, std::max(q.lddy, q.ldo));
+    if ((double)q.pixels * ld * es >= 2147483648.0) return best;
+    const int unit = cg / std::gcd(cg, V) * V;         // channels: whole groups, whole vectors
+    double best_cost = 0;
+    for (int width = unit;; width += unit) {
+        width = std::min(width, q.channels);
+        const int bx = width / V;
+        for (int threads = 256; threads <= kSlabThreads; threads *= 2) {
+            if (width > threads) continue;
+            const int rows = threads / bx, R = (q.pixels + rows - 1) / rows, need = R * (V * es / 4);
+            int i = 0;
+            while (i < N && regs[i] < need) ++i;
+            if (i == N) continue;
+            const double blocks = (q.channels + width - 1) / width, total = blocks * q.batch;
+            if (total >= 1e9) continue;
+            double cost = slab_cost(width * es, threads, regs[i], total, (double)q.pixels * width * es);
+            if (best.V && cost >= best_cost) continue;
+            best_cost = cost;
+            best.V = V; best.uni = cg % V == 0; best.threads = threads; best.regs = regs[i];
+            GnSlab &s = best.s;
+            s.N = q.batch; s.P = q.pixels; s.C = q.channels; s.G = q.groups; s.cg = cg;
+            s.width = width; s.blocks = (int)blocks; s.bx = bx; s.rows = rows; s.full = q.pixels / rows;
+            s.total = (unsigned)total; s.per = (int)((s.total + 7) / 8);
+            s.ldx = q.ldx; s.lddy = q.lddy; s.ldo = q.ldo;
+            s.dblocks = make_fastdiv((uint32_t)s.blocks); s.dbx = make_fastdiv((uint32_t)bx);
+        }
+        if (width == q.channels) break;
+    }
+    return best;
+}
+
+template <class F> void by_slab(int dtype, const SlabPlan &p, F &&f)
+{
+    const auto uni = [&](auto t, auto v) {
+        if (p.uni) f(t, v, std::true_type{});
+        else if constexpr (decltype(v)::value <= 4) f(t, v, std::false_type{});
+    };
+    if (dtype == kBF16) {
+        if (p.V == 8) uni(bf16_t{}, std::integral_constant<int, 8>{});
+        else uni(bf16_t{}, std::integral_constant<int, 4>{});
+    } else {
+        if (p.V == 4) uni(float{}, std::integral_constant<int, 4>{});
+        else uni(float{}, std::integral_constant<int, 2>{});
+    }
+}
+template <int I, int N, class F> void by_regs(int regs, const int (&all)[N], F &&f)
+{
+    if constexpr (I < N) {
+        if (regs == all[I]) f(std::integral_constant<int, I>{});
+        else by_regs<I + 1>(regs, all, f);
+    }
+}
+
 template <class F> void by_act(int act, F &&f)
 {
     if (act == kActRelu) f(std::integral_constant<int, kActRelu>{});
@@ -447,6 +827,20 @@ int launch_group_norm_fwd(const GroupNorm &q, const void *x, const void *gamma, 
                           hipStream_t st)
 {
     const int V = gn_vector(q.dtype, q.channels, (uintptr_t)x | (uintptr_t)y, q.ldx | q.ldo);
+    const SlabPlan slab = plan_slab(q, V, kFwdRegs);
+    if (slab.V) {
+        by_slab(q.dtype, slab, [&](auto t, auto v, auto uni) {
+            using T = decltype(t);
+            constexpr int W = decltype(v)::value;
+            by_regs<0>(slab.regs, kFwdRegs, [&](auto i) {
+                constexpr int R = kFwdRegs[decltype(i)::value] * 4 / (W * (int)sizeof(T));
+                const size_t lds = (size_t)slab.threads * (slab.uni ? 1 : W) * 8 + (size_t)std::max(slab.threads / 64, slab.s.width / slab.s.cg) * 16;
+                hipLaunchKernelGGL((gn_fwd_slab_kernel<T, W, decltype(uni)::value, R>), dim3(8u * (unsigned)slab.s.per), dim3(slab.threads), lds, st, slab.s,
+                                   static_cast<const T *>(x), static_cast<const T *>(gamma), static_cast<const T *>(beta), static_cast<T *>(y), mean, rstd, eps, q.act);
+            });
+        });
+        return launch_ok();
+    }
     GnShape s;
     if (!gn_shape(q, V, s)) return -1;
     double *part = static_cast<double *>(ws);
@@ -472,9 +866,28 @@ int launch_group_norm_bwd(const GroupNorm &q, const void *dy, const void *x, con
                           float *dgamma, float *dbeta, void *ws, hipStream_t st)
 {
     const int V = gn_vector(q.dtype, q.channels, (uintptr_t)x | (uintptr_t)dy | (uintptr_t)dx, q.ldx | q.lddy | q.ldo);
+    double *part = static_cast<double *>(ws);
+    const SlabPlan slab = plan_slab(q, V, kBwdRegs);
+    if (slab.V) {
+        by_slab(q.dtype, slab, [&](auto t, auto v, auto uni) {
+            using T = decltype(t);
+            constexpr int W = decltype(v)::value;
+            by_regs<0>(slab.regs, kBwdRegs, [&](auto i) {
+                constexpr int R = kBwdRegs[decltype(i)::value] * 4 / (W * (int)sizeof(T));
+                const size_t lds = (size_t)slab.threads * (W * 8 + 16);
+                by_act(q.act, [&](auto a) {
+                    hipLaunchKernelGGL((gn_bwd_slab_kernel<T, W, decltype(uni)::value, R, decltype(a)::value>), dim3(8u * (unsigned)slab.s.per), dim3(slab.threads), lds,
+                                       st, slab.s, static_cast<const T *>(dy), static_cast<const T *>(x), static_cast<const T *>(gamma), static_cast<const T *>(beta), mean,
+                                       rstd, static_cast<T *>(dx), part);
+                });
+            });
+        });
+        if (dgamma || dbeta)
+            hipLaunchKernelGGL(gn_param_grads_kernel, dim3(blocks_for(q.channels, 4)), dim3(kThreads), 0, st, part, (long)q.batch, q.channels, dgamma, dbeta);
+        return launch_ok();
+    }
     GnShape s;
     if (!gn_shape(q, V, s)) return -1;
-    double *part = static_cast<double *>(ws);
     float2 *coef = reinterpret_cast<float2 *>(static_cast<char *>(ws) + round256((size_t)s.N * s.chunks * s.C * 16));
     const unsigned blocks = (unsigned)s.N * s.chunks * s.cbs, group_blocks = blocks_for((size_t)s.N * s.G, kThreads / 64);
     by_vector(q.dtype, V, [&](auto t, auto v) {
