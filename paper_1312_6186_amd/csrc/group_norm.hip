@@ -522,13 +522,14 @@ __global__ __launch_bounds__(kSlabThreads) void gn_fwd_slab_kernel(GnSlab s, con
     // Waves share out the groups, or parts of their rows: sum x and sum x^2 in 64 bits
     const int waves = (int)blockDim.x / 64, wave = (int)threadIdx.x / 64, lane = (int)threadIdx.x & 63;
     const int parts = max(1, waves / groups), used = min(s.rows, s.P), gs = s.cg / (UNI ? V : 1);   // entries of a row of a group
+    const int across = gs >= 64 ? 6 : gs > 1 ? 32 - __clz(gs - 1) : 0;                              // lanes (a power of two) that share a row
     for (int base = 0; base < groups; base += waves) {
         const int part = groups < waves ? wave / groups : 0, g = groups < waves ? wave - part * groups : base + wave;
         double a = 0, b = 0;
         if (part < parts && g < groups) {
-            for (int r = part; r < used; r += parts) {
+            for (int r = (part << (6 - across)) + (lane >> across); r < used; r += parts << (6 - across)) {
                 const double cnt = (double)(pixels_of(s, r) * (UNI ? V : 1));
-                for (int q = lane; q < gs; q += 64) {
+                for (int q = lane & ((1 << across) - 1); q < gs; q += 64) {
                     const float2 p = lds[(r * s.bx) * S + g * gs + q];
                     const double cm = cnt * (double)p.x;
                     a += cm;
