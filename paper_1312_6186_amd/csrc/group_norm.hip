@@ -49,11 +49,11 @@ template <int ACT> __device__ __forceinline__ float activate(float z)
     if constexpr (ACT == kActSilu) return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f));
     return z;
 }
-// y = z s(z): y' = s (1 + z (1 - s))
+// y = z s(z): y' = s + z (s - s^2)
 __device__ __forceinline__ float silu_slope(float z)
 {
     const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f));
-    return s * __builtin_fmaf(z, 1.f - s, 1.f);
+    return __builtin_fmaf(z, __builtin_fmaf(-s, s, s), s);
 }
 
 // The next fp32 value below f, and the largest one that is not above t.
@@ -70,17 +70,16 @@ __device__ __forceinline__ float round_down(double t)
 
 // What the backward pass knows of one channel of one image, beside the mean of its group: z = (x - mean) * a + beta.
 template <int ACT> struct Channel {
-    float a, beta;     // ReLU: beta is the edge; z > 0 is x > edge where gamma > 0, and not x > edge (with the edge below t) where gamma < 0
+    float a, beta;     // ReLU: beta is the edge; z > 0 is x > edge where gamma >= 0, and not x > edge (with the edge below t) where gamma < 0
     bool falls;
     __device__ __forceinline__ void set(float mean, float rstd, float gamma, float b)
     {
-        a = rstd * gamma; beta = b; falls = false;
+        a = rstd * gamma; beta = b; falls = gamma < 0.f;
         if constexpr (ACT == kActRelu) {
             if (gamma == 0.f) {
                 beta = b > 0.f ? -__builtin_inff() : __builtin_inff();
             } else {
                 const double t = (double)mean - (double)b / ((double)rstd * (double)gamma);
-                falls = gamma < 0.f;
                 beta = round_down(t);
                 if (falls && (double)beta == t) beta = below(beta);
             }
@@ -416,7 +415,7 @@ __global__ __launch_bounds__(kThreads) void gn_bwd_apply_kernel(GnShape s, const
 struct GnSlab {
     int N, P, C, G, cg;
     int width, blocks;       // channels of a workgroup (whole groups, whole vectors), workgroups per image
-    int bx, rows, full;      // vectors of a row, pixels at a time, turns in which all rows lie in the image
+    int bx, rows, full, turns;   // vectors of a row, pixels at a time, turns in which all rows lie in the image, and in which some do
     unsigned total;          // workgroups with work
     int per;                 // of an XCD
     long ldx, lddy, ldo;
@@ -426,33 +425,35 @@ struct GnSlab {
 // Workgroups are dealt to the XCDs in turn; here each XCD gets a run of them, so that those that share the lines of an image's pixels share an L2.
 __device__ __forceinline__ unsigned slab_of(const GnSlab &s) { return (blockIdx.x & 7) * (unsigned)s.per + (blockIdx.x >> 3); }
 
-template <typename T, int V> __device__ __forceinline__ Pack<T, V> buf_pack(__amdgpu_buffer_rsrc_t rs, unsigned off)
+// The offset of a lane, and one of all lanes
+template <typename T, int V> __device__ __forceinline__ Pack<T, V> buf_pack(__amdgpu_buffer_rsrc_t rs, unsigned off, unsigned more)
 {
     Pack<T, V> r;
     if constexpr (sizeof(r) == 16) {
-        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, 0, 0);
+        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, (int)more, 0);
         __builtin_memcpy(&r, &v, 16);
     } else {
         static_assert(sizeof(r) == 8, "packs of 8 or 16 bytes");
-        const auto v = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)off, 0, 0);
+        const auto v = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)off, (int)more, 0);
         __builtin_memcpy(&r, &v, 8);
     }
     return r;
 }
-template <typename T, int V> __device__ __forceinline__ void buf_store_pack(__amdgpu_buffer_rsrc_t rs, unsigned off, const Pack<T, V> &r)
+template <typename T, int V> __device__ __forceinline__ void buf_store_pack(__amdgpu_buffer_rsrc_t rs, unsigned off, unsigned more, const Pack<T, V> &r)
 {
     if constexpr (sizeof(r) == 16) {
         u32x4 v;
         __builtin_memcpy(&v, &r, 16);
-        __builtin_amdgcn_raw_buffer_store_b128(v, rs, (int)off, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(v, rs, (int)off, (int)more, 0);
     } else {
         typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
         u32x2 v;
         __builtin_memcpy(&v, &r, 8);
-        __builtin_amdgcn_raw_buffer_store_b64(v, rs, (int)off, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b64(v, rs, (int)off, (int)more, 0);
     }
 }
-// Image n of a tensor as a range of bytes, from the workgroup's first channel on: loads behind it give zeros, stores behind it are dropped.
+// Image n of a tensor as a range of bytes, from the workgroup's first channel on: loads behind it give zeros, stores behind it are dropped.  Pixels
+// behind the last one are.
 template <typename T> __device__ __forceinline__ __amdgpu_buffer_rsrc_t image(const GnSlab &s, const T *p, long ld, unsigned n, int c_first)
 {
     const T *base = p + (size_t)n * s.P * ld + c_first;
@@ -465,9 +466,10 @@ __device__ __forceinline__ int pixels_of(const GnSlab &s, int r) { return s.full
 
 constexpr int kSlabThreads = 1024;
 
-template <typename T, int V, bool UNI, int R>
+// Without SILU: values below `low` become `low`, 0 for a ReLU and -inf for no activation.
+template <typename T, int V, bool UNI, int R, bool SILU>
 __global__ __launch_bounds__(kSlabThreads) void gn_fwd_slab_kernel(GnSlab s, const T *x, const T *gamma, const T *beta, T *y, float *mean_out, float *rstd_out,
-                                                                   float eps, int act)
+                                                                   float eps, float low)
 {
     constexpr int S = UNI ? 1 : V;     // statistics of a thread
     extern __shared__ __align__(16) char shared[];
@@ -484,7 +486,7 @@ __global__ __launch_bounds__(kSlabThreads) void gn_fwd_slab_kernel(GnSlab s, con
     const unsigned at = live ? (unsigned)((row * s.ldx + vec * V) * (long)sizeof(T)) : kNowhere;
     Pack<T, V> v[R];
 #pragma unroll
-    for (int k = 0; k < R; ++k) v[k] = buf_pack<T, V>(rx, live && k * s.rows + row < s.P ? at + k * step : kNowhere);
+    for (int k = 0; k < R; ++k) v[k] = buf_pack<T, V>(rx, at, k * step);
     float ga[V], be[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
@@ -493,12 +495,12 @@ __global__ __launch_bounds__(kSlabThreads) void gn_fwd_slab_kernel(GnSlab s, con
         be[e] = beta && live ? ldf(&beta[c]) : 0.f;
     }
     // of the thread's values (its channels together, or each): their mean, and the squares about it, by way of its first one
-    const int count = live ? pixels_of(s, row) : 0;
+    int count = live ? pixels_of(s, row) : 0;
     float m[S], m2[S], pivot[S];
 #pragma unroll
     for (int e = 0; e < S; ++e) { m[e] = m2[e] = 0.f; pivot[e] = ldf(&v[0].e[e]); }
     static_for<0, R>([&](auto k) ASGD_INLINE {
-        if (k < count) {
+        if (k < count) {   // by lanes: zeros behind the image are none of the values
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float d = ldf(&v[k].e[e]) - pivot[UNI ? 0 : e];
@@ -561,23 +563,22 @@ __global__ __launch_bounds__(kSlabThreads) void gn_fwd_slab_kernel(GnSlab s, con
         ga[e] *= st.y;
     }
     const auto ry = image(s, y, s.ldo, n, c_first);
-    const unsigned ostep = (unsigned)(s.rows * s.ldo * (long)sizeof(T)), oat = (unsigned)((row * s.ldo + vec * V) * (long)sizeof(T));
-    const auto store = [&](auto a) ASGD_INLINE {
-        static_for<0, R>([&](auto k) ASGD_INLINE {
-            if (k >= count) return;
-            forget(v[k]);
+    const unsigned ostep = (unsigned)(s.rows * s.ldo * (long)sizeof(T)), oat = live ? (unsigned)((row * s.ldo + vec * V) * (long)sizeof(T)) : kNowhere;
+    static_for<0, R>([&](auto k) ASGD_INLINE {
+        if (k >= s.turns) return;   // of all lanes
+        forget(v[k]);
 #pragma unroll
-            for (int e = 0; e < V; ++e) stf(&v[k].e[e], activate<decltype(a)::value>(__builtin_fmaf(ldf(&v[k].e[e]) - mean[UNI ? 0 : e], ga[e], be[e])));
-            buf_store_pack<T, V>(ry, oat + k * ostep, v[k]);
-        });
-    };
-    if (act == kActRelu) store(std::integral_constant<int, kActRelu>{});
-    else if (act == kActSilu) store(std::integral_constant<int, kActSilu>{});
-    else store(std::integral_constant<int, kActNone>{});
+        for (int e = 0; e < V; ++e) {
+            const float z = __builtin_fmaf(ldf(&v[k].e[e]) - mean[UNI ? 0 : e], ga[e], be[e]);
+            stf(&v[k].e[e], SILU ? activate<kActSilu>(z) : z < low ? low : z);
+        }
+        buf_store_pack<T, V>(ry, oat, k * ostep, v[k]);
+    });
 }
 
-// A and B of each image and channel go to part, for the parameters' gradients.
-template <typename T, int V, bool UNI, int R, int ACT>
+// A and B of each image and channel go to part, for the parameters' gradients.  With KEEP both tensors stay in registers; without, x does, and dy is read a
+// second time, from the memory-side cache: half the registers, and room for another workgroup that reads while this one computes.
+template <typename T, int V, bool UNI, int R, int ACT, bool KEEP>
 __global__ __launch_bounds__(kSlabThreads) void gn_bwd_slab_kernel(GnSlab s, const T *dy, const T *x, const T *gamma, const T *beta, const float *mean,
                                                                    const float *rstd, T *dx, double *part_out)
 {
@@ -585,6 +586,7 @@ __global__ __launch_bounds__(kSlabThreads) void gn_bwd_slab_kernel(GnSlab s, con
     extern __shared__ __align__(16) char shared[];
     float2 *lds = reinterpret_cast<float2 *>(shared);                                                // [rows][bx * V]
     double2 *sums = reinterpret_cast<double2 *>(shared + (size_t)blockDim.x * V * sizeof(float2));   // [thread]
+    float4 *consts = reinterpret_cast<float4 *>(sums + blockDim.x);                                  // [channel]
     const unsigned L = slab_of(s);
     if (L >= s.total) return;
     const unsigned n = fdiv(L, s.dblocks), cb = L - n * s.blocks;
@@ -593,36 +595,54 @@ __global__ __launch_bounds__(kSlabThreads) void gn_bwd_slab_kernel(GnSlab s, con
     const bool live = row < s.rows && vec * V < width;
     const auto rx = image(s, x, s.ldx, n, c_first), rd = image(s, dy, s.lddy, n, c_first);
     const unsigned xstep = (unsigned)(s.rows * s.ldx * (long)sizeof(T)), dstep = (unsigned)(s.rows * s.lddy * (long)sizeof(T));
-    const unsigned xat = (unsigned)((row * s.ldx + vec * V) * (long)sizeof(T)), dat = (unsigned)((row * s.lddy + vec * V) * (long)sizeof(T));
-    const int count = live ? pixels_of(s, row) : 0;
-    Pack<T, V> vx[R], vd[R];
+    const unsigned xat = live ? (unsigned)((row * s.ldx + vec * V) * (long)sizeof(T)) : kNowhere;
+    const unsigned dat = live ? (unsigned)((row * s.lddy + vec * V) * (long)sizeof(T)) : kNowhere;
+    // what belongs to a channel, asked for ahead of the tensors (loads return in order)
+    float own_mean = 0.f, own_rstd = 0.f, own_gamma = 1.f, own_beta = 0.f;
+    if (const int c = (int)threadIdx.x; c < width) {
+        const size_t i = (size_t)n * s.G + (c_first + c) / s.cg;
+        own_mean = mean[i]; own_rstd = rstd[i];
+        if (gamma) own_gamma = ldf(&gamma[c_first + c]);
+        if (beta) own_beta = ldf(&beta[c_first + c]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    constexpr int D = KEEP ? R : 6;    // packs of dy on their way
+    Pack<T, V> vx[R], vd[D];
+    const auto load_dy = [&](int k) ASGD_INLINE { return buf_pack<T, V>(rd, dat, k * dstep); };
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-        vx[k] = buf_pack<T, V>(rx, k < count ? xat + k * xstep : kNowhere);
-        vd[k] = buf_pack<T, V>(rd, k < count ? dat + k * dstep : kNowhere);
+        vx[k] = buf_pack<T, V>(rx, xat, k * xstep);
+        if (k < D) vd[k] = load_dy(k);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    if (const int c = (int)threadIdx.x; c < width) {   // the sign of gamma goes as that of the scale
+        Channel<ACT> one;
+        one.set(own_mean, own_rstd, own_gamma, own_beta);
+        consts[c] = make_float4(one.a, one.beta, own_mean, one.falls ? -own_rstd : own_rstd);
+    }
+    __syncthreads();
     Channel<ACT> ch[V];
     float m[S], r[S];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        const int c = live ? c_first + vec * V + e : 0;
-        const size_t i = (size_t)n * s.G + c / s.cg;
-        const float me = mean[i], re = rstd[i];
-        if (e < S) { m[e] = me; r[e] = re; }
-        ch[e].set(me, re, gamma ? ldf(&gamma[c]) : 1.f, beta ? ldf(&beta[c]) : 0.f);
+        const float4 k = consts[live ? vec * V + e : 0];
+        if (e < S) { m[e] = k.z; r[e] = __builtin_fabsf(k.w); }
+        ch[e].a = k.x; ch[e].beta = k.y; ch[e].falls = __float_as_uint(k.w) >> 31;
     }
     float sa[V], sb[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) sa[e] = sb[e] = 0.f;
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
+    static_for<0, R>([&](auto k) ASGD_INLINE {
+        if (k >= s.turns) return;
 #pragma unroll
         for (int e = 0; e < V; ++e) {   // zeros of dy behind the image add nothing
-            const float xv = ldf(&vx[k].e[e]), d = xv - m[UNI ? 0 : e], dz = ch[e].slope(ldf(&vd[k].e[e]), xv, d);
+            const float xv = ldf(&vx[k].e[e]), d = xv - m[UNI ? 0 : e], dz = ch[e].slope(ldf(&vd[k % D].e[e]), xv, d);
             sa[e] += dz;
             sb[e] = __builtin_fmaf(dz, d, sb[e]);
         }
-    }
+        if constexpr (k + D < R) vd[k % D] = load_dy(k + D);
+    });
+    if constexpr (!KEEP) static_for<0, D>([&](auto k) ASGD_INLINE { vd[k] = load_dy(k); });
     if (row < s.rows) {
 #pragma unroll
         for (int e = 0; e < V; ++e) lds[row * s.bx * V + vec * V + e] = make_float2(sa[e], sb[e] * r[UNI ? 0 : e]);
@@ -643,8 +663,7 @@ __global__ __launch_bounds__(kSlabThreads) void gn_bwd_slab_kernel(GnSlab s, con
         double2 t = sums[c];
         for (int p = 1; p < parts; ++p) { t.x += sums[p * pitch + c].x; t.y += sums[p * pitch + c].y; }
         reinterpret_cast<double2 *>(part_out)[(size_t)n * s.C + c_first + c] = t;
-        const double g = gamma ? (double)ldf(&gamma[c_first + c]) : 1.0;
-        sums[c] = make_double2(g * t.x, g * t.y);
+        sums[c] = make_double2((double)own_gamma * t.x, (double)own_gamma * t.y);
     }
     __syncthreads();
     float2 *coef = lds;
@@ -665,17 +684,19 @@ __global__ __launch_bounds__(kSlabThreads) void gn_bwd_slab_kernel(GnSlab s, con
         c2[e] = r[e] * r[e] * k.y;
     }
     const auto ro = image(s, dx, s.ldo, n, c_first);
-    const unsigned ostep = (unsigned)(s.rows * s.ldo * (long)sizeof(T)), oat = (unsigned)((row * s.ldo + vec * V) * (long)sizeof(T));
+    const unsigned ostep = (unsigned)(s.rows * s.ldo * (long)sizeof(T)), oat = live ? (unsigned)((row * s.ldo + vec * V) * (long)sizeof(T)) : kNowhere;
     static_for<0, R>([&](auto k) ASGD_INLINE {
-        if (k >= count) return;
+        if (k >= s.turns) return;   // of all lanes; what they store behind the image is dropped
+        Pack<T, V> o;
         forget(vx[k]);
-        forget(vd[k]);
+        if constexpr (KEEP) forget(vd[k]);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const float xv = ldf(&vx[k].e[e]), d = xv - m[UNI ? 0 : e], dz = ch[e].slope(ldf(&vd[k].e[e]), xv, d);
-            stf(&vd[k].e[e], __builtin_fmaf(-c2[UNI ? 0 : e], d, __builtin_fmaf(ch[e].a, dz, -c0[UNI ? 0 : e])));
+            const float xv = ldf(&vx[k].e[e]), d = xv - m[UNI ? 0 : e], dz = ch[e].slope(ldf(&vd[k % D].e[e]), xv, d);
+            stf(&o.e[e], __builtin_fmaf(-c2[UNI ? 0 : e], d, __builtin_fmaf(ch[e].a, dz, -c0[UNI ? 0 : e])));
         }
-        buf_store_pack<T, V>(ro, oat + k * ostep, vd[k]);
+        buf_store_pack<T, V>(ro, oat, k * ostep, o);
+        if constexpr (k + D < R) vd[k % D] = load_dy(k + D);
     });
 }
 
@@ -720,7 +741,7 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 // ---- slabs, host side
 
 // VGPRs that a thread's part of one tensor may take
-constexpr int kFwdRegs[] = {8, 16, 32, 72}, kBwdRegs[] = {8, 16, 36};
+constexpr int kFwdRegs[] = {8, 16, 32, 72}, kBwdRegs[] = {8, 16, 36, 72};
 
 // What a choice costs, for comparison alone.
 double slab_cost(int piece, int threads, int regs, double total, double bytes)
@@ -753,7 +774,7 @@ template <int N> SlabPlan plan_slab(const GroupNorm &q, int V, const int (&regs)
             const int rows = threads / bx, R = (q.pixels + rows - 1) / rows, need = R * (V * es / 4);
             int i = 0;
             while (i < N && regs[i] < need) ++i;
-            if (i == N) continue;
+            if (i == N || (double)(regs[i] / (V * es / 4)) * rows * ld * es >= 2147483648.0) continue;   // offsets of all turns
             const double blocks = (q.channels + width - 1) / width, total = blocks * q.batch;
             if (total >= 1e9) continue;
             double cost = slab_cost(width * es, threads, regs[i], total, (double)q.pixels * width * es);
@@ -762,7 +783,7 @@ template <int N> SlabPlan plan_slab(const GroupNorm &q, int V, const int (&regs)
             best.V = V; best.uni = cg % V == 0; best.threads = threads; best.regs = regs[i];
             GnSlab &s = best.s;
             s.N = q.batch; s.P = q.pixels; s.C = q.channels; s.G = q.groups; s.cg = cg;
-            s.width = width; s.blocks = (int)blocks; s.bx = bx; s.rows = rows; s.full = q.pixels / rows;
+            s.width = width; s.blocks = (int)blocks; s.bx = bx; s.rows = rows; s.full = q.pixels / rows; s.turns = R;
             s.total = (unsigned)total; s.per = (int)((s.total + 7) / 8);
             s.ldx = q.ldx; s.lddy = q.lddy; s.ldo = q.ldo;
             s.dblocks = make_fastdiv((uint32_t)s.blocks); s.dbx = make_fastdiv((uint32_t)bx);
@@ -836,8 +857,13 @@ int launch_group_norm_fwd(const GroupNorm &q, const void *x, const void *gamma, 
             by_regs<0>(slab.regs, kFwdRegs, [&](auto i) {
                 constexpr int R = kFwdRegs[decltype(i)::value] * 4 / (W * (int)sizeof(T));
                 const size_t lds = (size_t)slab.threads * (slab.uni ? 1 : W) * 8 + (size_t)std::max(slab.threads / 64, slab.s.width / slab.s.cg) * 16;
-                hipLaunchKernelGGL((gn_fwd_slab_kernel<T, W, decltype(uni)::value, R>), dim3(8u * (unsigned)slab.s.per), dim3(slab.threads), lds, st, slab.s,
-                                   static_cast<const T *>(x), static_cast<const T *>(gamma), static_cast<const T *>(beta), static_cast<T *>(y), mean, rstd, eps, q.act);
+                const auto go = [&](auto kernel) {
+                    hipLaunchKernelGGL(kernel, dim3(8u * (unsigned)slab.s.per), dim3(slab.threads), lds, st, slab.s, static_cast<const T *>(x),
+                                       static_cast<const T *>(gamma), static_cast<const T *>(beta), static_cast<T *>(y), mean, rstd, eps,
+                                       q.act == kActRelu ? 0.f : -INFINITY);
+                };
+                if (q.act == kActSilu) go(gn_fwd_slab_kernel<T, W, decltype(uni)::value, R, true>);
+                else go(gn_fwd_slab_kernel<T, W, decltype(uni)::value, R, false>);
             });
         });
         return launch_ok();
@@ -875,9 +901,9 @@ int launch_group_norm_bwd(const GroupNorm &q, const void *dy, const void *x, con
             constexpr int W = decltype(v)::value;
             by_regs<0>(slab.regs, kBwdRegs, [&](auto i) {
                 constexpr int R = kBwdRegs[decltype(i)::value] * 4 / (W * (int)sizeof(T));
-                const size_t lds = (size_t)slab.threads * (W * 8 + 16);
+                const size_t lds = (size_t)slab.threads * (W * 8 + 16) + (size_t)slab.s.width * 16;
                 by_act(q.act, [&](auto a) {
-                    hipLaunchKernelGGL((gn_bwd_slab_kernel<T, W, decltype(uni)::value, R, decltype(a)::value>), dim3(8u * (unsigned)slab.s.per), dim3(slab.threads), lds,
+                    hipLaunchKernelGGL((gn_bwd_slab_kernel<T, W, decltype(uni)::value, R, decltype(a)::value, (kBwdRegs[decltype(i)::value] <= 36)>), dim3(8u * (unsigned)slab.s.per), dim3(slab.threads), lds,
                                        st, slab.s, static_cast<const T *>(dy), static_cast<const T *>(x), static_cast<const T *>(gamma), static_cast<const T *>(beta), mean,
                                        rstd, static_cast<T *>(dx), part);
                 });
