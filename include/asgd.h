@@ -411,7 +411,8 @@ int asgd_accumulate(float *accum, const float *grads, size_t n, int first, void 
  * no other.  With no images or no pixels nothing is written.
  * Errors: ASGD_EINVAL (null, unknown dtype or act, eps not > 0 and finite,
  * overlap), ASGD_ESHAPE (negative sizes, channels not a multiple of groups,
- * strides below channels, more than 2^30 pixels or 2^31 groups in all),
+ * strides below channels or above 2^28 bytes, more than 2^30 pixels or 2^31
+ * groups in all),
  * ASGD_EALIGN, ASGD_EHIP. */
 typedef enum {
     ASGD_ACT_NONE = 0,

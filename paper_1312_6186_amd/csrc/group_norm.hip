@@ -93,16 +93,60 @@ template <int ACT> struct Channel {
     }
 };
 
+// The offset of a lane, and one of all lanes
+template <typename T, int V> __device__ __forceinline__ Pack<T, V> buf_pack(__amdgpu_buffer_rsrc_t rs, unsigned off, unsigned more)
+{
+    Pack<T, V> r;
+    if constexpr (sizeof(r) == 16) {
+        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, (int)more, 0);
+        __builtin_memcpy(&r, &v, 16);
+    } else if constexpr (sizeof(r) == 8) {
+        const auto v = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)off, (int)more, 0);
+        __builtin_memcpy(&r, &v, 8);
+    } else if constexpr (sizeof(r) == 4) {
+        const unsigned v = __builtin_amdgcn_raw_buffer_load_b32(rs, (int)off, (int)more, 0);
+        __builtin_memcpy(&r, &v, 4);
+    } else {
+        const unsigned short v = __builtin_amdgcn_raw_buffer_load_b16(rs, (int)off, (int)more, 0);
+        __builtin_memcpy(&r, &v, 2);
+    }
+    return r;
+}
+template <typename T, int V> __device__ __forceinline__ void buf_store_pack(__amdgpu_buffer_rsrc_t rs, unsigned off, unsigned more, const Pack<T, V> &r)
+{
+    if constexpr (sizeof(r) == 16) {
+        u32x4 v;
+        __builtin_memcpy(&v, &r, 16);
+        __builtin_amdgcn_raw_buffer_store_b128(v, rs, (int)off, (int)more, 0);
+    } else if constexpr (sizeof(r) == 8) {
+        typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+        u32x2 v;
+        __builtin_memcpy(&v, &r, 8);
+        __builtin_amdgcn_raw_buffer_store_b64(v, rs, (int)off, (int)more, 0);
+    } else if constexpr (sizeof(r) == 4) {
+        unsigned v;
+        __builtin_memcpy(&v, &r, 4);
+        __builtin_amdgcn_raw_buffer_store_b32(v, rs, (int)off, (int)more, 0);
+    } else {
+        unsigned short v;
+        __builtin_memcpy(&v, &r, 2);
+        __builtin_amdgcn_raw_buffer_store_b16(v, rs, (int)off, (int)more, 0);
+    }
+}
+constexpr unsigned kNowhere = 0x80000000u;   // ranges are shorter (checked on the host): loads from there give zeros, stores to there are dropped
+
+// ---- two passes over a tensor, by chunks of pixels
+
 struct GnShape {
     int N, P, C, G, cg;
     long ldx, lddy, ldo;
     int chunks, pc;          // chunks of pc pixels
     int cbs, bx, rows;       // channel blocks of bx vectors, pixels that a workgroup takes at a time
-    FastDiv dcbs, dchunks;
+    FastDiv dcbs, dchunks, dbx;
 };
 
-// Where a thread of the passes over the tensor works.
-struct Place { int n, chunk, p0, p1, row, vec, c0; bool live; };
+// Where a thread of the passes over the tensor works: channels c_first .. c_first + width of `pixels` pixels from p0 on.
+struct Place { int n, chunk, p0, pixels, turns, row, vec, c_first, width; bool live; };
 template <int V> __device__ __forceinline__ Place place(const GnShape &s)
 {
     Place w;
@@ -110,90 +154,105 @@ template <int V> __device__ __forceinline__ Place place(const GnShape &s)
     w.n = (int)fdiv(r, s.dchunks);
     w.chunk = (int)(r - (unsigned)w.n * s.chunks);
     w.p0 = w.chunk * s.pc;
-    w.p1 = min(s.P, w.p0 + s.pc);
-    w.row = (int)threadIdx.x / s.bx;
+    w.pixels = min(s.pc, s.P - w.p0);
+    w.turns = (w.pixels + s.rows - 1) / s.rows;
+    w.row = (int)fdiv(threadIdx.x, s.dbx);
     w.vec = (int)threadIdx.x - w.row * s.bx;
-    w.c0 = ((int)cb * s.bx + w.vec) * V;
-    w.live = w.row < s.rows && w.c0 < s.C;
+    w.c_first = (int)cb * s.bx * V;
+    w.width = min(s.bx * V, s.C - w.c_first);
+    w.live = w.row < s.rows && w.vec * V < w.width;
     return w;
 }
-
-template <typename T, int V> __device__ __forceinline__ Pack<T, V> load_pack(const T *p) { return *reinterpret_cast<const Pack<T, V> *>(p); }
+// The chunk's part of a tensor, from the block's first channel on, as ranges of bytes that start at a turn: pixels behind the chunk lie behind their end.
+template <typename T> struct ChunkOf {
+    const char *base; long bytes, pace; unsigned at, step;
+    template <int V> __device__ __forceinline__ void set(const GnShape &s, const Place &w, const T *p, long ld, std::integral_constant<int, V>)
+    {
+        base = reinterpret_cast<const char *>(p + ((size_t)w.n * s.P + w.p0) * ld + w.c_first);
+        const unsigned odd = (unsigned)(reinterpret_cast<uintptr_t>(base) & 3);    // ranges start at whole words
+        base -= odd;
+        bytes = ((w.pixels - 1) * ld + s.C - w.c_first) * (long)sizeof(T) + odd;
+        pace = s.rows * ld * (long)sizeof(T);
+        step = (unsigned)pace;
+        at = w.live ? (unsigned)((w.row * ld + w.vec * V) * (long)sizeof(T)) + odd : kNowhere;
+    }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t from(int turn) const
+    {
+        const long skip = turn * pace, left = bytes - skip;
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base) + skip, 0, (int)min(left, 0x7fffffffL), 0x00020000);
+    }
+};
 
 // The two sums of every channel over the rows of a workgroup, in 64 bits: from each thread's V pairs (u, v) and what add() makes of them.
 template <int V, class F>
-__device__ __forceinline__ void channel_sums(const GnShape &s, const Place &w, const float (&u)[V], const float (&v)[V], double *part, F &&add)
+__device__ __forceinline__ void channel_sums(const GnShape &s, const Place &w, float2 *lds, const float (&u)[V], const float (&v)[V], double *part, F &&add)
 {
-    __shared__ float2 lds[kThreads * V];
     __shared__ double2 sums[kThreads];
-    const int width = s.bx * V;
+    const int pitch = s.bx * V;
     if (w.row < s.rows) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) lds[w.row * width + w.vec * V + e] = make_float2(u[e], v[e]);
+        for (int e = 0; e < V; ++e) lds[w.row * pitch + w.vec * V + e] = make_float2(u[e], v[e]);
     }
     __syncthreads();
-    const int c_first = w.c0 - w.vec * V;     // of the channel block
-    double *out = part + (((size_t)w.n * s.chunks + w.chunk) * s.C + c_first) * 2;
-    const int used = min(s.rows, w.p1 - w.p0);
-    const int split = width < kThreads ? kThreads / width : 1;   // threads that share a channel
-    for (int base = 0; base < width; base += kThreads) {         // the same number of turns in all threads
-        const int q = (int)threadIdx.x / (split > 1 ? width : kThreads), ch = split > 1 ? (int)threadIdx.x - q * width : base + (int)threadIdx.x;
-        double2 t = make_double2(0, 0);
-        if (q < split && ch < width)
-            for (int r = q; r < used; r += split) add(t, lds[r * width + ch], r);
-        if (split > 1) {
-            sums[threadIdx.x] = t;
-            __syncthreads();
-            if (q == 0)
-                for (int k = 1; k < split; ++k) { t.x += sums[k * width + ch].x; t.y += sums[k * width + ch].y; }
+    double2 *out = reinterpret_cast<double2 *>(part) + ((size_t)w.n * s.chunks + w.chunk) * s.C + w.c_first;
+    const int used = min(s.rows, w.pixels);
+    if (pitch >= kThreads) {      // a thread takes whole channels
+        for (int c = (int)threadIdx.x; c < w.width; c += kThreads) {
+            double2 t = make_double2(0, 0);
+            for (int r = 0; r < used; ++r) add(t, lds[r * pitch + c], r);
+            out[c] = t;
         }
-        if (q == 0 && ch < width && c_first + ch < s.C) { out[2 * ch] = t.x; out[2 * ch + 1] = t.y; }
+        return;
+    }
+    const int split = kThreads / pitch, q = (int)threadIdx.x / pitch, c = (int)threadIdx.x - q * pitch;   // threads that share a channel
+    double2 t = make_double2(0, 0);
+    if (q < split)
+        for (int r = q; r < used; r += split) add(t, lds[r * pitch + c], r);
+    sums[threadIdx.x] = t;
+    __syncthreads();
+    if ((int)threadIdx.x < w.width) {
+        for (int k = 1; k < split; ++k) { t.x += sums[k * pitch + c].x; t.y += sums[k * pitch + c].y; }
+        out[c] = t;
     }
 }
 
 // Sums of x and x^2 of each image, chunk and channel.
 template <typename T, int V> __global__ __launch_bounds__(kThreads) void gn_fwd_sums_kernel(GnShape s, const T *x, double *part)
 {
+    __shared__ float2 lds[kThreads * V];
     const Place w = place<V>(s);
-    float mean[V], m2[V];
+    ChunkOf<T> cx;
+    cx.set(s, w, x, s.ldx, std::integral_constant<int, V>{});
+    const int count = w.live ? w.turns - (w.row + (w.turns - 1) * s.rows < w.pixels ? 0 : 1) : 0;
+    const Pack<T, V> first = buf_pack<T, V>(cx.from(0), cx.at, 0);
+    float pivot[V], mean[V], m2[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) mean[e] = m2[e] = 0.f;
-    if (w.live && w.p0 + w.row < w.p1) {
-        const T *px = x + ((size_t)w.n * s.P + w.p0 + w.row) * s.ldx + w.c0;
-        const size_t step = (size_t)s.rows * s.ldx;
-        float pivot[V];
-        const Pack<T, V> first = load_pack<T, V>(px);
+    for (int e = 0; e < V; ++e) { pivot[e] = ldf(&first.e[e]); mean[e] = m2[e] = 0.f; }
+    for (int k = 0; k < w.turns; k += kUnroll) {
+        const auto rx = cx.from(k);
+        Pack<T, V> v[kUnroll];
 #pragma unroll
-        for (int e = 0; e < V; ++e) pivot[e] = ldf(&first.e[e]);
-        int count = 0;
-        for (int p = w.p0 + w.row; p < w.p1; p += kUnroll * s.rows, px += kUnroll * step) {
-            Pack<T, V> v[kUnroll];
+        for (int u = 0; u < kUnroll; ++u) v[u] = buf_pack<T, V>(rx, cx.at, u * cx.step);
 #pragma unroll
-            for (int k = 0; k < kUnroll; ++k)
-                if (p + k * (long)s.rows < w.p1) v[k] = load_pack<T, V>(px + k * step);
+        for (int u = 0; u < kUnroll; ++u) {
+            if (k + u >= count) continue;
 #pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
-                if (p + k * (long)s.rows >= w.p1) continue;
-                ++count;
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float d = ldf(&v[k].e[e]) - pivot[e];
-                    mean[e] += d;
-                    m2[e] = __builtin_fmaf(d, d, m2[e]);
-                }
+            for (int e = 0; e < V; ++e) {
+                const float d = ldf(&v[u].e[e]) - pivot[e];
+                mean[e] += d;
+                m2[e] = __builtin_fmaf(d, d, m2[e]);
             }
         }
-        const float inv = 1.f / (float)count;
-#pragma unroll
-        for (int e = 0; e < V; ++e) {   // of this thread's values: their mean, and the squares about it
-            const float d = mean[e] * inv;
-            m2[e] = __builtin_fmaf(-mean[e], d, m2[e]);
-            mean[e] = pivot[e] + d;
-        }
     }
-    const int span = w.p1 - w.p0;
-    channel_sums<V>(s, w, mean, m2, part, [&](double2 &t, float2 v, int r) ASGD_INLINE {
-        const double n = (double)((span - r + s.rows - 1) / s.rows), m = (double)v.x;
+    const float inv = count ? 1.f / (float)count : 0.f;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {   // of this thread's values: their mean, and the squares about it
+        const float d = mean[e] * inv;
+        m2[e] = __builtin_fmaf(-mean[e], d, m2[e]);
+        mean[e] = pivot[e] + d;
+    }
+    channel_sums<V>(s, w, lds, mean, m2, part, [&](double2 &t, float2 v, int r) ASGD_INLINE {
+        const double n = (double)((w.pixels - r + s.rows - 1) / s.rows), m = (double)v.x;
         t.x = __builtin_fma(n, m, t.x);
         t.y += __builtin_fma(n * m, m, (double)v.y);
     });
@@ -213,70 +272,94 @@ __device__ __forceinline__ float2 group_stats(double a, double b, double M, floa
     return make_float2((float)m, (float)(1.0 / __builtin_sqrt((var > 0 ? var : var == var ? 0.0 : var) + (double)eps)));
 }
 
-// One wave per image and group: its mean and rstd.
-__global__ __launch_bounds__(kThreads) void gn_fwd_stats_kernel(GnShape s, const double *part, float eps, float *mean, float *rstd)
+// The two sums of image and group i over its chunks and channels by `team` threads (64 to 1024 of a workgroup), each channel times weight(c); done(a, b) in
+// one of them.
+constexpr int kTeamThreads = 1024;
+template <class W, class F>
+__device__ __forceinline__ void group_sums(const GnShape &s, const FastDiv &dcg, const double *part, unsigned i, int team, W &&weight, F &&done)
 {
-    const unsigned i = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-    if (i >= (unsigned)s.N * (unsigned)s.G) return;
-    const unsigned n = i / s.G, g = i - n * s.G;
-    const double *p = part + ((size_t)n * s.chunks * s.C + (size_t)g * s.cg) * 2;
+    __shared__ double2 waves[kTeamThreads / 64];
+    const int j0 = (int)threadIdx.x & (team - 1);
+    const bool live = i < (unsigned)s.N * (unsigned)s.G;
     double a = 0, b = 0;
-    const long entries = (long)s.chunks * s.cg;
-    for (long j = threadIdx.x & 63; j < entries; j += 64) {
-        const long k = j / s.cg, c = j - k * s.cg;
-        const double *q = p + ((size_t)k * s.C + c) * 2;
-        a += q[0]; b += q[1];
+    if (live) {
+        const unsigned n = i / s.G, g = i - n * s.G;
+        const double2 *p = reinterpret_cast<const double2 *>(part) + (size_t)n * s.chunks * s.C + (size_t)g * s.cg;
+        const int entries = s.chunks * s.cg;
+#pragma unroll 4
+        for (int j = j0; j < entries; j += team) {
+            const int k = (int)fdiv((unsigned)j, dcg), c = j - k * s.cg;
+            const double2 q = p[(size_t)k * s.C + c];
+            const double w = weight((int)g * s.cg + c);
+            a = __builtin_fma(w, q.x, a); b = __builtin_fma(w, q.y, b);
+        }
     }
     wave_sum(a, b);
-    if ((threadIdx.x & 63) == 0) {
+    if (team > 64) {
+        if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = make_double2(a, b);
+        __syncthreads();
+        if (j0 == 0)
+            for (int k = 1; k < team / 64; ++k) { a += waves[(threadIdx.x >> 6) + k].x; b += waves[(threadIdx.x >> 6) + k].y; }
+    }
+    if (live && j0 == 0) done(a, b);
+}
+
+__global__ __launch_bounds__(kTeamThreads) void gn_fwd_stats_kernel(GnShape s, FastDiv dcg, const double *part, int team, float eps, float *mean, float *rstd)
+{
+    const unsigned i = (blockIdx.x * blockDim.x + threadIdx.x) / (unsigned)team;
+    group_sums(s, dcg, part, i, team, [](int) { return 1.0; }, [&](double a, double b) ASGD_INLINE {
         const float2 st = group_stats(a, b, (double)s.P * s.cg, eps);
         mean[i] = st.x;
         rstd[i] = st.y;
-    }
+    });
 }
 
+// What belongs to a channel is worked out once a workgroup and goes through LDS.
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void gn_fwd_apply_kernel(GnShape s, const T *x, const T *gamma, const T *beta, const float *mean, const float *rstd, T *y)
 {
+    extern __shared__ __align__(16) char shared[];
+    float4 *consts = reinterpret_cast<float4 *>(shared);   // [width]
     const Place w = place<V>(s);
-    if (!w.live) return;
+    for (int c = (int)threadIdx.x; c < w.width; c += kThreads) {
+        const size_t i = (size_t)w.n * s.G + (w.c_first + c) / s.cg;
+        consts[c] = make_float4(mean[i], rstd[i] * (gamma ? ldf(&gamma[w.c_first + c]) : 1.f), beta ? ldf(&beta[w.c_first + c]) : 0.f, 0.f);
+    }
+    __syncthreads();
     float m[V], a[V], b[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        const int c = w.c0 + e, i = w.n * s.G + c / s.cg;
-        m[e] = mean[i];
-        a[e] = rstd[i] * (gamma ? ldf(&gamma[c]) : 1.f);
-        b[e] = beta ? ldf(&beta[c]) : 0.f;
+        const float4 k = consts[w.live ? w.vec * V + e : 0];
+        m[e] = k.x; a[e] = k.y; b[e] = k.z;
     }
-    const size_t at = (size_t)w.n * s.P + w.p0 + w.row;
-    const T *px = x + at * s.ldx + w.c0;
-    T *py = y + at * s.ldo + w.c0;
-    const size_t step = (size_t)s.rows * s.ldx, ostep = (size_t)s.rows * s.ldo;
-    for (int p = w.p0 + w.row; p < w.p1; p += kUnroll * s.rows, px += kUnroll * step, py += kUnroll * ostep) {
+    ChunkOf<T> cx, cy;
+    cx.set(s, w, x, s.ldx, std::integral_constant<int, V>{});
+    cy.set(s, w, y, s.ldo, std::integral_constant<int, V>{});
+    for (int k = 0; k < w.turns; k += kUnroll) {
+        const auto rx = cx.from(k), ry = cy.from(k);
         Pack<T, V> v[kUnroll];
 #pragma unroll
-        for (int k = 0; k < kUnroll; ++k)
-            if (p + k * (long)s.rows < w.p1) v[k] = load_pack<T, V>(px + k * step);
+        for (int u = 0; u < kUnroll; ++u) v[u] = buf_pack<T, V>(rx, cx.at, u * cx.step);
 #pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-            if (p + k * (long)s.rows >= w.p1) continue;
+        for (int u = 0; u < kUnroll; ++u) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) stf(&v[k].e[e], activate<ACT>(__builtin_fmaf(ldf(&v[k].e[e]) - m[e], a[e], b[e])));
-            *reinterpret_cast<Pack<T, V> *>(py + k * ostep) = v[k];
+            for (int e = 0; e < V; ++e) stf(&v[u].e[e], activate<ACT>(__builtin_fmaf(ldf(&v[u].e[e]) - m[e], a[e], b[e])));
+            buf_store_pack<T, V>(ry, cy.at, u * cy.step, v[u]);
         }
     }
 }
 
-template <typename T, int V, int ACT>
-__device__ __forceinline__ void load_channels(const GnShape &s, const Place &w, const T *gamma, const T *beta, const float *mean, const float *rstd,
-                                              Channel<ACT> (&ch)[V], float (&m)[V], float (&r)[V])
+// a, beta (ReLU: the edge), mean and rstd of channel c; the sign of gamma goes as that of rstd.
+template <typename T, int ACT>
+__device__ __forceinline__ float4 channel_consts(const T *gamma, const T *beta, float mean, float rstd, int c)
 {
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-        const int c = w.c0 + e, i = w.n * s.G + c / s.cg;
-        m[e] = mean[i]; r[e] = rstd[i];
-        ch[e].set(m[e], r[e], gamma ? ldf(&gamma[c]) : 1.f, beta ? ldf(&beta[c]) : 0.f);
-    }
+    Channel<ACT> one;
+    one.set(mean, rstd, gamma ? ldf(&gamma[c]) : 1.f, beta ? ldf(&beta[c]) : 0.f);
+    return make_float4(one.a, one.beta, mean, one.falls ? -rstd : rstd);
+}
+template <int ACT> __device__ __forceinline__ void take(Channel<ACT> &ch, float &m, float &r, const float4 &k)
+{
+    ch.a = k.x; ch.beta = k.y; m = k.z; r = __builtin_fabsf(k.w); ch.falls = __float_as_uint(k.w) >> 31;
 }
 
 // A and B of each image, chunk and channel.
@@ -284,48 +367,56 @@ template <typename T, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void gn_bwd_sums_kernel(GnShape s, const T *dy, const T *x, const T *gamma, const T *beta, const float *mean,
                                                                const float *rstd, double *part)
 {
+    extern __shared__ __align__(16) char shared[];
+    float4 *consts = reinterpret_cast<float4 *>(shared);     // [width], and after them the threads' sums
     const Place w = place<V>(s);
-    float sa[V], sb[V];
+    for (int c = (int)threadIdx.x; c < w.width; c += kThreads) {
+        const size_t i = (size_t)w.n * s.G + (w.c_first + c) / s.cg;
+        consts[c] = channel_consts<T, ACT>(gamma, beta, mean[i], rstd[i], w.c_first + c);
+    }
+    __syncthreads();
+    Channel<ACT> ch[V];
+    float m[V], r[V], sa[V], sb[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) sa[e] = sb[e] = 0.f;
-    if (w.live) {
-        Channel<ACT> ch[V];
-        float m[V], r[V];
-        load_channels<T, V, ACT>(s, w, gamma, beta, mean, rstd, ch, m, r);
-        const size_t at = (size_t)w.n * s.P + w.p0 + w.row;
-        const T *px = x + at * s.ldx + w.c0, *pd = dy + at * s.lddy + w.c0;
-        const size_t xstep = (size_t)s.rows * s.ldx, dstep = (size_t)s.rows * s.lddy;
-        for (int p = w.p0 + w.row; p < w.p1; p += kUnroll * s.rows, px += kUnroll * xstep, pd += kUnroll * dstep) {
-            Pack<T, V> vx[kUnroll], vd[kUnroll];
+    for (int e = 0; e < V; ++e) { take(ch[e], m[e], r[e], consts[w.live ? w.vec * V + e : 0]); sa[e] = sb[e] = 0.f; }
+    ChunkOf<T> cx, cd;
+    cx.set(s, w, x, s.ldx, std::integral_constant<int, V>{});
+    cd.set(s, w, dy, s.lddy, std::integral_constant<int, V>{});
+    for (int k = 0; k < w.turns; k += kUnroll) {
+        const auto rd = cd.from(k), rx = cx.from(k);
+        Pack<T, V> vx[kUnroll], vd[kUnroll];
 #pragma unroll
-            for (int k = 0; k < kUnroll; ++k)
-                if (p + k * (long)s.rows < w.p1) { vx[k] = load_pack<T, V>(px + k * xstep); vd[k] = load_pack<T, V>(pd + k * dstep); }
-#pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
-                if (p + k * (long)s.rows >= w.p1) continue;
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float xv = ldf(&vx[k].e[e]), d = xv - m[e], dz = ch[e].slope(ldf(&vd[k].e[e]), xv, d);
-                    sa[e] += dz;
-                    sb[e] = __builtin_fmaf(dz, d, sb[e]);
-                }
-            }
+        for (int u = 0; u < kUnroll; ++u) {
+            vx[u] = buf_pack<T, V>(rx, cx.at, u * cx.step);
+            vd[u] = buf_pack<T, V>(rd, cd.at, u * cd.step);
         }
 #pragma unroll
-        for (int e = 0; e < V; ++e) sb[e] *= r[e];
+        for (int u = 0; u < kUnroll; ++u) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {   // zeros of dy behind the chunk add nothing
+                const float xv = ldf(&vx[u].e[e]), d = xv - m[e], dz = ch[e].slope(ldf(&vd[u].e[e]), xv, d);
+                sa[e] += dz;
+                sb[e] = __builtin_fmaf(dz, d, sb[e]);
+            }
+        }
     }
-    channel_sums<V>(s, w, sa, sb, part, [](double2 &t, float2 v, int) ASGD_INLINE { t.x += (double)v.x; t.y += (double)v.y; });
+#pragma unroll
+    for (int e = 0; e < V; ++e) sb[e] *= r[e];
+    __syncthreads();
+    channel_sums<V>(s, w, reinterpret_cast<float2 *>(shared), sa, sb, part,
+                    [](double2 &t, float2 v, int) ASGD_INLINE { t.x += (double)v.x; t.y += (double)v.y; });
 }
 
 // dgamma and dbeta of four channels, 64 threads each over `entries` (images and chunks of them).
-__device__ __forceinline__ void param_grads(const double *part, long entries, int C, int first, float *dgamma, float *dbeta)
+__global__ __launch_bounds__(kThreads) void gn_param_grads_kernel(const double *part, long entries, int C, float *dgamma, float *dbeta)
 {
     __shared__ double2 lds[kThreads];
-    const int c = first + ((int)threadIdx.x & 3);
+    const int c = (int)blockIdx.x * 4 + ((int)threadIdx.x & 3);
     double2 t = make_double2(0, 0);
     if (c < C) {
+#pragma unroll 4
         for (long j = threadIdx.x >> 2; j < entries; j += kThreads / 4) {
-            const double2 v = *reinterpret_cast<const double2 *>(part + ((size_t)j * C + c) * 2);
+            const double2 v = reinterpret_cast<const double2 *>(part)[(size_t)j * C + c];
             t.x += v.x; t.y += v.y;
         }
     }
@@ -340,70 +431,63 @@ __device__ __forceinline__ void param_grads(const double *part, long entries, in
         if (dgamma) dgamma[c] = (float)lds[threadIdx.x].y;
     }
 }
-__global__ __launch_bounds__(kThreads) void gn_param_grads_kernel(const double *part, long entries, int C, float *dgamma, float *dbeta)
-{
-    param_grads(part, entries, C, (int)blockIdx.x * 4, dgamma, dbeta);
-}
 
-// The first workgroups: one wave per image and group, (sum gamma A) / M and (sum gamma B) / M into coef.  The others: the parameters' gradients.
+// (sum gamma A) / M and (sum gamma B) / M of each image and group.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void gn_bwd_stats_kernel(GnShape s, const double *part, const T *gamma, float2 *coef, float *dgamma, float *dbeta,
-                                                                unsigned group_blocks)
+__global__ __launch_bounds__(kTeamThreads) void gn_bwd_stats_kernel(GnShape s, FastDiv dcg, const double *part, const T *gamma, int team, float2 *coef)
 {
-    if (blockIdx.x >= group_blocks) {
-        param_grads(part, (long)s.N * s.chunks, s.C, (int)(blockIdx.x - group_blocks) * 4, dgamma, dbeta);
-        return;
-    }
-    const unsigned i = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-    if (i >= (unsigned)s.N * (unsigned)s.G) return;
-    const unsigned n = i / s.G, g = i - n * s.G;
-    const double *p = part + ((size_t)n * s.chunks * s.C + (size_t)g * s.cg) * 2;
-    double a = 0, b = 0;
-    const long entries = (long)s.chunks * s.cg;
-    for (long j = threadIdx.x & 63; j < entries; j += 64) {
-        const long k = j / s.cg, c = j - k * s.cg;
-        const double *q = p + ((size_t)k * s.C + c) * 2;
-        const double w = gamma ? (double)ldf(&gamma[g * s.cg + c]) : 1.0;
-        a = __builtin_fma(w, q[0], a); b = __builtin_fma(w, q[1], b);
-    }
-    wave_sum(a, b);
-    const double M = (double)s.P * s.cg;
-    if ((threadIdx.x & 63) == 0) coef[i] = make_float2((float)(a / M), (float)(b / M));
+    const unsigned i = (blockIdx.x * blockDim.x + threadIdx.x) / (unsigned)team;
+    group_sums(s, dcg, part, i, team, [&](int c) ASGD_INLINE { return gamma ? (double)ldf(&gamma[c]) : 1.0; }, [&](double a, double b) ASGD_INLINE {
+        const double M = (double)s.P * s.cg;
+        coef[i] = make_float2((float)(a / M), (float)(b / M));
+    });
 }
 
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void gn_bwd_apply_kernel(GnShape s, const T *dy, const T *x, const T *gamma, const T *beta, const float *mean,
                                                                 const float *rstd, const float2 *coef, T *dx)
 {
+    extern __shared__ __align__(16) char shared[];
+    float4 *consts = reinterpret_cast<float4 *>(shared);                   // [width]
     const Place w = place<V>(s);
-    if (!w.live) return;
+    float2 *more = reinterpret_cast<float2 *>(consts + s.bx * V);          // [width]
+    for (int c = (int)threadIdx.x; c < w.width; c += kThreads) {
+        const size_t i = (size_t)w.n * s.G + (w.c_first + c) / s.cg;
+        const float r = rstd[i];
+        const float2 k = coef[i];
+        consts[c] = channel_consts<T, ACT>(gamma, beta, mean[i], r, w.c_first + c);
+        more[c] = make_float2(r * k.x, r * r * k.y);
+    }
+    __syncthreads();
     Channel<ACT> ch[V];
     float m[V], c0[V], c2[V];   // dx = a * dz - c0 - c2 * (x - mean)
-    load_channels<T, V, ACT>(s, w, gamma, beta, mean, rstd, ch, m, c2);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        const float2 k = coef[w.n * s.G + (w.c0 + e) / s.cg];
-        c0[e] = c2[e] * k.x;
-        c2[e] = c2[e] * c2[e] * k.y;
+        const int c = w.live ? w.vec * V + e : 0;
+        float r;
+        take(ch[e], m[e], r, consts[c]);
+        c0[e] = more[c].x; c2[e] = more[c].y;
     }
-    const size_t at = (size_t)w.n * s.P + w.p0 + w.row;
-    const T *px = x + at * s.ldx + w.c0, *pd = dy + at * s.lddy + w.c0;
-    T *po = dx + at * s.ldo + w.c0;
-    const size_t xstep = (size_t)s.rows * s.ldx, dstep = (size_t)s.rows * s.lddy, ostep = (size_t)s.rows * s.ldo;
-    for (int p = w.p0 + w.row; p < w.p1; p += kUnroll * s.rows, px += kUnroll * xstep, pd += kUnroll * dstep, po += kUnroll * ostep) {
+    ChunkOf<T> cx, cd, co;
+    cx.set(s, w, x, s.ldx, std::integral_constant<int, V>{});
+    cd.set(s, w, dy, s.lddy, std::integral_constant<int, V>{});
+    co.set(s, w, dx, s.ldo, std::integral_constant<int, V>{});
+    for (int k = 0; k < w.turns; k += kUnroll) {
+        const auto rd = cd.from(k), ro = co.from(k), rx = cx.from(k);
         Pack<T, V> vx[kUnroll], vd[kUnroll];
 #pragma unroll
-        for (int k = 0; k < kUnroll; ++k)
-            if (p + k * (long)s.rows < w.p1) { vx[k] = load_pack<T, V>(px + k * xstep); vd[k] = load_pack<T, V>(pd + k * dstep); }
+        for (int u = 0; u < kUnroll; ++u) {
+            vx[u] = buf_pack<T, V>(rx, cx.at, u * cx.step);
+            vd[u] = buf_pack<T, V>(rd, cd.at, u * cd.step);
+        }
 #pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-            if (p + k * (long)s.rows >= w.p1) continue;
+        for (int u = 0; u < kUnroll; ++u) {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float xv = ldf(&vx[k].e[e]), d = xv - m[e], dz = ch[e].slope(ldf(&vd[k].e[e]), xv, d);
-                stf(&vd[k].e[e], __builtin_fmaf(-c2[e], d, __builtin_fmaf(ch[e].a, dz, -c0[e])));
+                const float xv = ldf(&vx[u].e[e]), d = xv - m[e], dz = ch[e].slope(ldf(&vd[u].e[e]), xv, d);
+                stf(&vd[u].e[e], __builtin_fmaf(-c2[e], d, __builtin_fmaf(ch[e].a, dz, -c0[e])));
             }
-            *reinterpret_cast<Pack<T, V> *>(po + k * ostep) = vd[k];
+            buf_store_pack<T, V>(ro, co.at, u * co.step, vd[u]);
         }
     }
 }
@@ -425,33 +509,6 @@ struct GnSlab {
 // Workgroups are dealt to the XCDs in turn; here each XCD gets a run of them, so that those that share the lines of an image's pixels share an L2.
 __device__ __forceinline__ unsigned slab_of(const GnSlab &s) { return (blockIdx.x & 7) * (unsigned)s.per + (blockIdx.x >> 3); }
 
-// The offset of a lane, and one of all lanes
-template <typename T, int V> __device__ __forceinline__ Pack<T, V> buf_pack(__amdgpu_buffer_rsrc_t rs, unsigned off, unsigned more)
-{
-    Pack<T, V> r;
-    if constexpr (sizeof(r) == 16) {
-        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, (int)more, 0);
-        __builtin_memcpy(&r, &v, 16);
-    } else {
-        static_assert(sizeof(r) == 8, "packs of 8 or 16 bytes");
-        const auto v = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)off, (int)more, 0);
-        __builtin_memcpy(&r, &v, 8);
-    }
-    return r;
-}
-template <typename T, int V> __device__ __forceinline__ void buf_store_pack(__amdgpu_buffer_rsrc_t rs, unsigned off, unsigned more, const Pack<T, V> &r)
-{
-    if constexpr (sizeof(r) == 16) {
-        u32x4 v;
-        __builtin_memcpy(&v, &r, 16);
-        __builtin_amdgcn_raw_buffer_store_b128(v, rs, (int)off, (int)more, 0);
-    } else {
-        typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-        u32x2 v;
-        __builtin_memcpy(&v, &r, 8);
-        __builtin_amdgcn_raw_buffer_store_b64(v, rs, (int)off, (int)more, 0);
-    }
-}
 // Image n of a tensor as a range of bytes, from the workgroup's first channel on: loads behind it give zeros, stores behind it are dropped.  Pixels
 // behind the last one are.
 template <typename T> __device__ __forceinline__ __amdgpu_buffer_rsrc_t image(const GnSlab &s, const T *p, long ld, unsigned n, int c_first)
@@ -459,8 +516,6 @@ template <typename T> __device__ __forceinline__ __amdgpu_buffer_rsrc_t image(co
     const T *base = p + (size_t)n * s.P * ld + c_first;
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(base), 0, (int)(((s.P - 1) * ld + s.C - c_first) * (long)sizeof(T)), 0x00020000);
 }
-constexpr unsigned kNowhere = 0x80000000u;   // images are shorter (checked on the host)
-
 // How many of the rows r, r + rows, ... lie in the image.
 __device__ __forceinline__ int pixels_of(const GnSlab &s, int r) { return s.full + (s.full * s.rows + r < s.P ? 1 : 0); }
 
@@ -625,9 +680,9 @@ __global__ __launch_bounds__(kSlabThreads) void gn_bwd_slab_kernel(GnSlab s, con
     float m[S], r[S];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        const float4 k = consts[live ? vec * V + e : 0];
-        if (e < S) { m[e] = k.z; r[e] = __builtin_fabsf(k.w); }
-        ch[e].a = k.x; ch[e].beta = k.y; ch[e].falls = __float_as_uint(k.w) >> 31;
+        float me, re;
+        take(ch[e], me, re, consts[live ? vec * V + e : 0]);
+        if (e < S) { m[e] = me; r[e] = re; }
     }
     float sa[V], sb[V];
 #pragma unroll
@@ -702,13 +757,15 @@ __global__ __launch_bounds__(kSlabThreads) void gn_bwd_slab_kernel(GnSlab s, con
 
 // ---- host side
 
-// Chunks of pixels: 2048 workgroups in all (eight a CU), of at least 32 KiB of a tensor each.
+// Chunks of pixels of 16 to 128 KiB of a tensor, small ones only as far as it takes 1024 workgroups (four a CU): what a workgroup does once (the constants
+// of its channels, the sums of its threads) is as much as 10 KiB take.  us, least 32 KiB and 2048 workgroups / as here:
+// CHUNKFIGS
 void gn_chunks(int batch, int pixels, int channels, int dtype, int &chunks, int &pc)
 {
     const long bytes = (long)channels * (long)dtype_size(dtype);
-    const long least = std::max<long>(1, (32768 + bytes - 1) / bytes);
-    long want = std::min<long>((2048 + batch - 1) / batch, (pixels + least - 1) / least);
-    want = std::max<long>(1, want);
+    const auto per = [&](long size) { return std::max<long>(1, (size + bytes - 1) / bytes); };   // pixels
+    const long most = ((long)pixels + per(16 << 10) - 1) / per(16 << 10), least = ((long)pixels + per(128 << 10) - 1) / per(128 << 10);
+    const long want = std::max(least, std::min<long>(most, (1024 + batch - 1) / batch));
     pc = (int)((pixels + want - 1) / want);
     chunks = (pixels + pc - 1) / pc;
 }
@@ -731,9 +788,25 @@ bool gn_shape(const GroupNorm &q, int V, GnShape &s)
     s.cbs = (cv + kThreads - 1) / kThreads;
     s.bx = (cv + s.cbs - 1) / s.cbs;
     s.rows = kThreads / s.bx;
+    // the offsets of kUnroll turns fit 31 bits
+    const long ld = std::max(q.ldx, std::max(q.lddy, q.ldo)) * (long)dtype_size(q.dtype);
+    s.rows = (int)std::max<long>(1, std::min<long>(s.rows, (1L << 28) / ld));
     s.dcbs = make_fastdiv((uint32_t)s.cbs);
     s.dchunks = make_fastdiv((uint32_t)s.chunks);
+    s.dbx = make_fastdiv((uint32_t)s.bx);
     return (double)s.N * s.chunks * s.cbs < 2147483648.0 && (double)s.N * s.G < 2147483648.0;
+}
+
+// Threads for the sums of one image and group: 64 where they have up to eight entries each, up to a whole workgroup.
+struct Teams { int team, threads; unsigned blocks; };
+Teams teams(const GnShape &s)
+{
+    const long entries = (long)s.chunks * s.cg;
+    Teams t;
+    t.team = entries <= 512 ? 64 : entries <= 2048 ? 256 : kTeamThreads;
+    t.threads = std::max(kThreads, t.team);
+    t.blocks = blocks_for((size_t)s.N * s.G, (unsigned)(t.threads / t.team));
+    return t;
 }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
@@ -880,9 +953,10 @@ int launch_group_norm_fwd(const GroupNorm &q, const void *x, const void *gamma, 
         constexpr int W = decltype(v)::value;
         const T *xx = static_cast<const T *>(x);
         hipLaunchKernelGGL((gn_fwd_sums_kernel<T, W>), dim3(blocks), dim3(kThreads), 0, st, s, xx, part);
-        hipLaunchKernelGGL(gn_fwd_stats_kernel, dim3(blocks_for((size_t)s.N * s.G, kThreads / 64)), dim3(kThreads), 0, st, s, part, eps, mean, rstd);
+        const Teams t3 = teams(s);
+        hipLaunchKernelGGL(gn_fwd_stats_kernel, dim3(t3.blocks), dim3(t3.threads), 0, st, s, make_fastdiv((uint32_t)s.cg), part, t3.team, eps, mean, rstd);
         by_act(q.act, [&](auto a) {
-            hipLaunchKernelGGL((gn_fwd_apply_kernel<T, W, decltype(a)::value>), dim3(blocks), dim3(kThreads), 0, st, s, xx, static_cast<const T *>(gamma),
+            hipLaunchKernelGGL((gn_fwd_apply_kernel<T, W, decltype(a)::value>), dim3(blocks), dim3(kThreads), (size_t)s.bx * W * 16, st, s, xx, static_cast<const T *>(gamma),
                                static_cast<const T *>(beta), mean, rstd, static_cast<T *>(y));
         });
     });
@@ -916,19 +990,22 @@ int launch_group_norm_bwd(const GroupNorm &q, const void *dy, const void *x, con
     GnShape s;
     if (!gn_shape(q, V, s)) return -1;
     float2 *coef = reinterpret_cast<float2 *>(static_cast<char *>(ws) + round256((size_t)s.N * s.chunks * s.C * 16));
-    const unsigned blocks = (unsigned)s.N * s.chunks * s.cbs, group_blocks = blocks_for((size_t)s.N * s.G, kThreads / 64);
+    const unsigned blocks = (unsigned)s.N * s.chunks * s.cbs;
     by_vector(q.dtype, V, [&](auto t, auto v) {
         using T = decltype(t);
         constexpr int W = decltype(v)::value;
         const T *xx = static_cast<const T *>(x), *dd = static_cast<const T *>(dy), *gg = static_cast<const T *>(gamma), *bb = static_cast<const T *>(beta);
         by_act(q.act, [&](auto a) {
             constexpr int ACT = decltype(a)::value;
-            hipLaunchKernelGGL((gn_bwd_sums_kernel<T, W, ACT>), dim3(blocks), dim3(kThreads), 0, st, s, dd, xx, gg, bb, mean, rstd, part);
-            hipLaunchKernelGGL(gn_bwd_stats_kernel<T>, dim3(group_blocks + (dgamma || dbeta ? blocks_for(s.C, 4) : 0)), dim3(kThreads), 0, st, s, part, gg, coef,
-                               dgamma, dbeta, group_blocks);
-            hipLaunchKernelGGL((gn_bwd_apply_kernel<T, W, ACT>), dim3(blocks), dim3(kThreads), 0, st, s, dd, xx, gg, bb, mean, rstd, coef, static_cast<T *>(dx));
+            const size_t sums_lds = std::max<size_t>((size_t)s.bx * W * 16, (size_t)kThreads * W * 8);
+            hipLaunchKernelGGL((gn_bwd_sums_kernel<T, W, ACT>), dim3(blocks), dim3(kThreads), sums_lds, st, s, dd, xx, gg, bb, mean, rstd, part);
+            const Teams t3 = teams(s);
+            hipLaunchKernelGGL(gn_bwd_stats_kernel<T>, dim3(t3.blocks), dim3(t3.threads), 0, st, s, make_fastdiv((uint32_t)s.cg), part, gg, t3.team, coef);
+            hipLaunchKernelGGL((gn_bwd_apply_kernel<T, W, ACT>), dim3(blocks), dim3(kThreads), (size_t)s.bx * W * 24, st, s, dd, xx, gg, bb, mean, rstd, coef, static_cast<T *>(dx));
         });
     });
+    if (dgamma || dbeta)
+        hipLaunchKernelGGL(gn_param_grads_kernel, dim3(blocks_for(q.channels, 4)), dim3(kThreads), 0, st, part, (long)s.N * s.chunks, q.channels, dgamma, dbeta);
     return launch_ok();
 }
 
