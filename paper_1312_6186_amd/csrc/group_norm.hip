@@ -816,53 +816,70 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 // VGPRs that a thread's part of one tensor may take
 constexpr int kFwdRegs[] = {8, 16, 32, 72}, kBwdRegs[] = {8, 16, 36, 72};
 
-// What a choice costs, for comparison alone.
-double slab_cost(int piece, int threads, int regs, double total, double bytes)
-{
-    // lines of 128 bytes that a piece of a pixel touches, over what it uses of them; rounds over the CUs
-    const double lines = (piece + 127) / 128 * 128.0 / piece;
-    const int fit = std::max(1, std::min(2048 / threads, (regs <= 16 ? 2048 : 1024) / threads));
-    const double rounds = std::ceil(total / (256.0 * fit));
-    return rounds * fit * bytes * lines;
-}
-
 struct SlabPlan { int V = 0, uni = 0, threads = 0, regs = 0; GnSlab s; };
 
-// The slabs of a call; V = 0 where there are none: vectors below 8 bytes, images that do not fit, strides beyond 32-bit offsets.
-template <int N> SlabPlan plan_slab(const GroupNorm &q, int V, const int (&regs)[N])
+// us that a pass takes in n slabs of `bytes` of a tensor each, in rounds over the CUs: a start, what a thread does with its `regs` VGPRs of values one after
+// the other, and memory and arithmetic of all workgroups, which overlap in part.  piece: bytes of a pixel.  Fitted to 1970 choices of width and threads for 161
+// shapes (15 % off on average).  Of those shapes its choice is 2.2 % slower than the best one on average, 34 % at most, and the choice between slabs and chunks
+// (chunk_us) included 2.6 and 35 %.
+double slab_us(bool bwd, int act, int es, int threads, int regs, int piece, double n, double bytes)
+{
+    const int waves = regs <= 8 ? 7 : regs <= 16 && !bwd ? 5 : 4, fit = std::max(1, std::min(2048 / threads, waves * 4 / (threads / 64)));   // on a CU
+    const double lines = 1 + 0.3 * ((128 - piece % 128) % 128) / 128.0 * std::min(1.0, 128.0 / piece);
+    const double moved = bytes * lines * (!bwd ? 2 : regs <= 36 ? 3 : 4), values = regs * 4.0 / es;
+    const double ops = (bwd ? 3.1 : 1) * (act == kActSilu ? 1.75 : 1);
+    const auto round = [&](double k) {   // ns of k workgroups
+        const double each = std::ceil(k / 256);
+        const double memory = each * moved / std::min(72.0, 5200 / std::min(256.0, k)), work = each * values * threads * 0.092 * ops;
+        return 3500 + 12 * each * threads / 64 + 1.6 * values * ops + std::max(memory, work) + 0.16 * std::min(memory, work);
+    };
+    const double all = 256.0 * fit, whole = std::floor(n / all), rest = n - whole * all;
+    return 2 + (whole * round(all) + (rest > 0 ? round(rest) : 0)) / 1000;
+}
+// us of the two passes by chunks, fitted to the same shapes (11 % off on average).
+double chunk_us(bool bwd, double bytes) { return (bwd ? 14 : 10) + bytes * (bwd ? 5 : 3) / 5.0e6; }
+
+// The slabs of a call; V = 0 where there are none: vectors below 8 bytes, images that do not fit, strides beyond 32-bit offsets, or chunks are faster.
+template <int N> SlabPlan plan_slab(const GroupNorm &q, int vector, bool bwd, const int (&regs)[N])
 {
     SlabPlan best;
     const int es = (int)dtype_size(q.dtype), cg = q.channels / q.groups;
-    if (cg % V && V * es == 16 && es == 2) V /= 2;     // per-channel statistics for four channels at most
-    if (V * es < 8) return best;
     const long ld = std::max(q.ldx, std::max(q.lddy, q.ldo));
     if ((double)q.pixels * ld * es >= 2147483648.0) return best;
-    const int unit = cg / std::gcd(cg, V) * V;         // channels: whole groups, whole vectors
-    double best_cost = 0;
-    for (int width = unit;; width += unit) {
-        width = std::min(width, q.channels);
-        const int bx = width / V;
-        for (int threads = 256; threads <= kSlabThreads; threads *= 2) {
-            if (width > threads) continue;
-            const int rows = threads / bx, R = (q.pixels + rows - 1) / rows, need = R * (V * es / 4);
-            int i = 0;
-            while (i < N && regs[i] < need) ++i;
-            if (i == N || (double)(regs[i] / (V * es / 4)) * rows * ld * es >= 2147483648.0) continue;   // offsets of all turns
-            const double blocks = (q.channels + width - 1) / width, total = blocks * q.batch;
-            if (total >= 1e9) continue;
-            double cost = slab_cost(width * es, threads, regs[i], total, (double)q.pixels * width * es);
-            if (best.V && cost >= best_cost) continue;
-            best_cost = cost;
-            best.V = V; best.uni = cg % V == 0; best.threads = threads; best.regs = regs[i];
-            GnSlab &s = best.s;
-            s.N = q.batch; s.P = q.pixels; s.C = q.channels; s.G = q.groups; s.cg = cg;
-            s.width = width; s.blocks = (int)blocks; s.bx = bx; s.rows = rows; s.full = q.pixels / rows; s.turns = R;
-            s.total = (unsigned)total; s.per = (int)((s.total + 7) / 8);
-            s.ldx = q.ldx; s.lddy = q.lddy; s.ldo = q.ldo;
-            s.dblocks = make_fastdiv((uint32_t)s.blocks); s.dbx = make_fastdiv((uint32_t)bx);
+    double best_us = 0;
+    int best_width = 0;
+    for (int V = vector; V * es >= 8; V /= 2) {
+        if (cg % V && V > 4) continue;                     // per-channel statistics for four channels at most
+        const int unit = cg / std::gcd(cg, V) * V;         // channels: whole groups, whole vectors
+        for (int j = 1, last = 0; !last; j += j < 4 ? 1 : j & (j - 1) ? (j + 3) / 3 : j / 2) {   // 1, 2, 3, 4, 6, 8, 12, 16, ...
+            const int width = (long)unit * j >= q.channels ? q.channels : unit * j, bx = width / V;
+            last = width == q.channels;
+            for (int threads = 256; threads <= kSlabThreads; threads *= 2) {
+                if (width > threads) continue;
+                const int rows = threads / bx, R = (q.pixels + rows - 1) / rows, need = R * (V * es / 4);
+                int i = 0;
+                while (i < N && regs[i] < need) ++i;
+                if (i == N || (double)(regs[i] / (V * es / 4)) * rows * ld * es >= 2147483648.0) continue;   // offsets of all turns
+                const double total = (double)((q.channels + width - 1) / width) * q.batch;
+                if (total >= 1e9) continue;
+                const double us = slab_us(bwd, q.act, es, threads, need, width * es, total, (double)q.pixels * width * es);
+                if (best.V && us >= best_us) continue;
+                best_us = us; best_width = width;
+                best.V = V; best.threads = threads; best.regs = regs[i];
+            }
         }
-        if (width == q.channels) break;
+        if (cg % V == 0) break;
     }
+    if (best.V && best_us > 1.15 * chunk_us(bwd, (double)q.batch * q.pixels * q.channels * es)) best.V = 0;
+    if (!best.V) return best;
+    best.uni = cg % best.V == 0;
+    GnSlab &s = best.s;
+    s.N = q.batch; s.P = q.pixels; s.C = q.channels; s.G = q.groups; s.cg = cg;
+    s.width = best_width; s.blocks = (q.channels + best_width - 1) / best_width;
+    s.bx = best_width / best.V; s.rows = best.threads / s.bx; s.full = q.pixels / s.rows; s.turns = (q.pixels + s.rows - 1) / s.rows;
+    s.total = (unsigned)s.blocks * (unsigned)q.batch; s.per = (int)((s.total + 7) / 8);
+    s.ldx = q.ldx; s.lddy = q.lddy; s.ldo = q.ldo;
+    s.dblocks = make_fastdiv((uint32_t)s.blocks); s.dbx = make_fastdiv((uint32_t)s.bx);
     return best;
 }
 
@@ -922,7 +939,7 @@ int launch_group_norm_fwd(const GroupNorm &q, const void *x, const void *gamma, 
                           hipStream_t st)
 {
     const int V = gn_vector(q.dtype, q.channels, (uintptr_t)x | (uintptr_t)y, q.ldx | q.ldo);
-    const SlabPlan slab = plan_slab(q, V, kFwdRegs);
+    const SlabPlan slab = plan_slab(q, V, false, kFwdRegs);
     if (slab.V) {
         by_slab(q.dtype, slab, [&](auto t, auto v, auto uni) {
             using T = decltype(t);
@@ -968,7 +985,7 @@ int launch_group_norm_bwd(const GroupNorm &q, const void *dy, const void *x, con
 {
     const int V = gn_vector(q.dtype, q.channels, (uintptr_t)x | (uintptr_t)dy | (uintptr_t)dx, q.ldx | q.lddy | q.ldo);
     double *part = static_cast<double *>(ws);
-    const SlabPlan slab = plan_slab(q, V, kBwdRegs);
+    const SlabPlan slab = plan_slab(q, V, true, kBwdRegs);
     if (slab.V) {
         by_slab(q.dtype, slab, [&](auto t, auto v, auto uni) {
             using T = decltype(t);
