@@ -124,14 +124,14 @@ def _check(rc):
 
 
 def _ptr(t):
-    return ctypes.c_void_p(t.data_ptr()) if t is not None else ctypes.c_void_p(0)
+    return t.data_ptr() if t is not None else None
 
 
 def _stream(stream):
     if stream is None:
         import torch
         stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream if isinstance(stream, int) else stream.cuda_stream)
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def layer_descs(layers):

@@ -22,7 +22,9 @@ namespace asgd {
 // A tensor is cut into tiles of 1024 aligned 16-byte pieces, counted from the piece that holds its first element (tensors are slices of a
 // vector: they start and end anywhere).  Each thread takes four pieces of a tile.
 constexpr int kTilePieces = 1024;
-constexpr int kClipBlocks = 2048;   // eight workgroups of four waves a CU
+// Workgroups of a pass.  Fewer leave memory waiting, more add the partial sums up more often (us, 161 tensors of 100 M elements in bf16 clipped with 512,
+// 1024, 1536 workgroups: 161, 144, 139; 62 M parameters updated with 512, 1024, 1536, 2048: 286, 272, 277, 283).
+constexpr int kClipBlocks = 1536, kUpdateBlocks = 1024;
 
 static inline uint64_t tensor_tiles(const void *p, size_t count, int es)
 {
@@ -33,36 +35,44 @@ static inline uint64_t tensor_tiles(const void *p, size_t count, int es)
 
 template <typename T> struct Piece {
     static constexpr int E = 16 / (int)sizeof(T);
-    union { uint4 u; T e[E]; };
+    union { u32x4 u; T e[E]; };
 };
 
 // The four pieces of tile `tile` of tensor q that belong to this thread, elements outside the tensor as zeros.  body(piece, first element, whole).
-template <typename T, class F> __device__ __forceinline__ void each_piece(const TensorTable &t, int q, unsigned tile, F &&body)
+template <typename T, bool ONCE, class F> __device__ __forceinline__ void each_piece(const TensorTable &t, int q, unsigned tile, F &&body)
 {
     constexpr int E = Piece<T>::E;
     const uintptr_t addr = reinterpret_cast<uintptr_t>(t.in[q]);
-    const long head = (long)(addr & 15) / (long)sizeof(T), count = (long)t.count[q];
+    const long head = (long)(addr & 15) / (long)sizeof(T), count = (long)t.count[q], start = (long)tile * kTilePieces * E - head;
     const T *base = reinterpret_cast<const T *>(addr & ~(uintptr_t)15);
     const long first = (long)tile * kTilePieces + threadIdx.x;
     Piece<T> v[4];
+    if (start >= 0 && start + kTilePieces * E <= count) {   // a tile inside the tensor: all loads at once
 #pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const u32x4 *p = reinterpret_cast<const u32x4 *>(base + (first + u * 256) * E);
+            if constexpr (ONCE) v[u].u = __builtin_nontemporal_load(p);
+            else v[u].u = *p;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) body(v[u], (first + u * 256) * E - head, true);
+        return;
+    }
     for (int u = 0; u < 4; ++u) {
         const long at = (first + u * 256) * E - head;   // element of the tensor at the piece's start
-        if (at >= 0 && at + E <= count) {
-            v[u].u = *reinterpret_cast<const uint4 *>(base + (first + u * 256) * E);
+        if (at >= count) return;
+        const bool whole = at >= 0 && at + E <= count;
+        if (whole) {
+            v[0].u = *reinterpret_cast<const u32x4 *>(base + (first + u * 256) * E);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const bool in = at + e >= 0 && at + e < count;
-                v[u].e[e] = (T)0.f;
-                if (in) v[u].e[e] = base[(first + u * 256) * E + e];
+                v[0].e[e] = (T)0.f;
+                if (in) v[0].e[e] = base[(first + u * 256) * E + e];
             }
         }
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const long at = (first + u * 256) * E - head;
-        body(v[u], at, at >= 0 && at + E <= count);
+        body(v[0], at, whole);
     }
 }
 
@@ -105,7 +115,7 @@ __device__ __forceinline__ int tensor_of(const TensorTable &t, unsigned tile)   
     return lo;
 }
 
-template <typename T> __global__ __launch_bounds__(256) void square_sums_kernel(TensorTable t, double *partials)
+template <typename T, bool ONCE> __global__ __launch_bounds__(256) void square_sums_kernel(TensorTable t, double *partials)
 {
     __shared__ double lds[4];
     const unsigned tiles = t.start[t.n];
@@ -115,7 +125,7 @@ template <typename T> __global__ __launch_bounds__(256) void square_sums_kernel(
         int q = tensor_of(t, begin);
         for (unsigned tile = begin; tile < end; ++tile) {
             while (tile >= t.start[q + 1]) ++q;
-            each_piece<T>(t, q, tile - t.start[q], [&](const Piece<T> &v, long, bool) ASGD_INLINE {
+            each_piece<T, ONCE>(t, q, tile - t.start[q], [&](const Piece<T> &v, long, bool) ASGD_INLINE {
 #pragma unroll
                 for (int e = 0; e < Piece<T>::E; ++e) {
                     const double x = (double)ldf(&v.e[e]);
@@ -153,11 +163,11 @@ template <typename T> __global__ __launch_bounds__(256) void clip_kernel(TensorT
         T *out = static_cast<T *>(t.out[q]);
         const bool aligned = ((reinterpret_cast<uintptr_t>(t.in[q]) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
         const long count = (long)t.count[q];
-        each_piece<T>(t, q, tile - t.start[q], [&](Piece<T> v, long at, bool whole) ASGD_INLINE {
+        each_piece<T, false>(t, q, tile - t.start[q], [&](Piece<T> v, long at, bool whole) ASGD_INLINE {
 #pragma unroll
             for (int e = 0; e < E; ++e) stf(&v.e[e], clipped(ldf(&v.e[e]), f));
             if (whole && aligned) {
-                *reinterpret_cast<uint4 *>(out + at) = v.u;
+                __builtin_nontemporal_store(v.u, reinterpret_cast<u32x4 *>(out + at));   // what is still to be read stays in the cache (164 us with ordinary stores, 144)
             } else {
 #pragma unroll
                 for (int e = 0; e < E; ++e)
@@ -236,10 +246,20 @@ __global__ __launch_bounds__(256) void clipped_update_scalar_kernel(float *w, fl
 
 // ---- host side
 
-size_t norm_partials(int n_tensors) { return (size_t)kClipBlocks + (size_t)(n_tensors + kTableTensors - 1) / kTableTensors; }
+size_t norm_partials(int n_tensors)
+{
+    const size_t tables = ((size_t)n_tensors + kTableTensors - 1) / kTableTensors;
+    return tables <= 4 ? std::max<size_t>(1, tables) * kClipBlocks : std::max<size_t>(4 * kClipBlocks, tables * 256);
+}
 
 // Calls launch(table, workgroups, their first partial sum) for every kTableTensors tensors; the number of partial sums, or -1.
-// Workgroups are dealt out by the tables' tiles, at least one a table.
+// A table has a launch of its own, of up to kClipBlocks workgroups; from five tables on they share four times as many (at least 256 a table), which bounds
+// the partial sums that every workgroup of the second pass adds up.
+static unsigned table_blocks(uint64_t tiles, int tables)
+{
+    const uint64_t most = tables <= 4 ? kClipBlocks : std::max(256, 4 * kClipBlocks / tables);
+    return (unsigned)std::max<uint64_t>(1, std::min(tiles, most));
+}
 template <class F> static long each_table(const void *const *in, void *const *out, const size_t *counts, int n, int dtype, F &&launch)
 {
     const int es = (int)dtype_size(dtype);
@@ -248,6 +268,7 @@ template <class F> static long each_table(const void *const *in, void *const *ou
         total += tensor_tiles(in[i], counts[i], es);
         if (total > 0xffffffffu) return -1;
     }
+    const int tables = (n + kTableTensors - 1) / kTableTensors;
     long first = 0;
     for (int i = 0; i < n;) {
         TensorTable t;
@@ -261,8 +282,7 @@ template <class F> static long each_table(const void *const *in, void *const *ou
         }
         if (t.n == 0) continue;
         t.start[t.n] = (unsigned)tiles;
-        const uint64_t share = total > (uint64_t)kClipBlocks ? tiles * kClipBlocks / total : tiles;
-        const unsigned blocks = (unsigned)(share ? share : 1);
+        const unsigned blocks = table_blocks(tiles, tables);
         launch(t, blocks, first);
         if (launch_ok() != 0) return -1;
         first += blocks;
@@ -270,17 +290,26 @@ template <class F> static long each_table(const void *const *in, void *const *ou
     return first;
 }
 
-static long launch_square_sums(const void *const *grads, const size_t *counts, int n, int dtype, double *partials, hipStream_t s)
+// once: by non-temporal loads
+static long launch_square_sums(const void *const *grads, const size_t *counts, int n, int dtype, bool once, double *partials, hipStream_t s)
 {
     return each_table(grads, nullptr, counts, n, dtype, [&](const TensorTable &t, unsigned blocks, long first) {
-        if (dtype == kBF16) hipLaunchKernelGGL(square_sums_kernel<bf16_t>, dim3(blocks), dim3(256), 0, s, t, partials + first);
-        else hipLaunchKernelGGL(square_sums_kernel<float>, dim3(blocks), dim3(256), 0, s, t, partials + first);
+        const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, s, t, partials + first); };
+        if (dtype == kBF16) once ? go(square_sums_kernel<bf16_t, true>) : go(square_sums_kernel<bf16_t, false>);
+        else once ? go(square_sums_kernel<float, true>) : go(square_sums_kernel<float, false>);
     });
 }
 
+// Whether a gradient that is read for its norm alone is left out of the memory-side cache: where it is too large for whoever reads it next to find it there.
+// us with ordinary / non-temporal loads, fp32 elements: 16 M 14.5 / 14.7, 28 M 23.7 / 22.1, 44 M 36.3 / 32.4, 62 M 48.2 / 41.6.  Up to 192 MiB (50 M) the
+// ordinary ones are kept all the same: an update of 44 M finds a gradient that is in the cache.
+bool norm_streams(size_t bytes) { return bytes > ((size_t)192 << 20); }
+
 int launch_grad_norm(const void *const *grads, const size_t *counts, int n, int dtype, float *norm, double *partials, hipStream_t s)
 {
-    const long np = launch_square_sums(grads, counts, n, dtype, partials, s);
+    size_t bytes = 0;
+    for (int i = 0; i < n; ++i) bytes += counts[i] * dtype_size(dtype);
+    const long np = launch_square_sums(grads, counts, n, dtype, norm_streams(bytes), partials, s);
     if (np < 0) return -1;
     hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(256), 0, s, partials, (int)np, norm);
     return launch_ok();
@@ -288,7 +317,7 @@ int launch_grad_norm(const void *const *grads, const size_t *counts, int n, int 
 
 int launch_clip(const void *const *grads, void *const *out, const size_t *counts, int n, int dtype, float max_norm, float *norm, double *partials, hipStream_t s)
 {
-    const long np = launch_square_sums(grads, counts, n, dtype, partials, s);
+    const long np = launch_square_sums(grads, counts, n, dtype, false, partials, s);
     if (np < 0) return -1;
     if (np == 0) {
         if (!norm) return 0;
@@ -311,7 +340,7 @@ static int launch_update_clipped_t(float *w, float *v, const float *g, size_t n,
     if (aligned) {
         const size_t tiles = (n / 4 + 1023) / 1024;
         if (tiles > 0x7fffffffu) return -1;
-        const unsigned blocks = (unsigned)std::max<size_t>(1, std::min<size_t>(tiles, kClipBlocks));
+        const unsigned blocks = (unsigned)std::max<size_t>(1, std::min<size_t>(tiles, kUpdateBlocks));
         const auto go = [&](auto kernel) {
             hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, s, w, v, g, n, (unsigned)tiles, lr, mu, wd, partials, np, max_norm, norm, copy);
         };
@@ -328,7 +357,7 @@ int launch_update_clipped(float *w, float *v, const float *g, size_t n, float lr
                           double *partials, hipStream_t s)
 {
     const void *grads[1] = {g};
-    const long np = launch_square_sums(grads, &n, 1, kF32, partials, s);
+    const long np = launch_square_sums(grads, &n, 1, kF32, false, partials, s);
     if (np < 0) return -1;
     if (!copy) return launch_update_clipped_t<0>(w, v, g, n, lr, mu, wd, max_norm, norm, nullptr, partials, (int)np, s);
     if (dst_dtype == kBF16) return launch_update_clipped_t<2>(w, v, g, n, lr, mu, wd, max_norm, norm, copy, partials, (int)np, s);
