@@ -407,11 +407,12 @@ int asgd_accumulate(float *accum, const float *grads, size_t n, int first, void 
  *             aligned; its contents do not matter, and calls that may overlap on
  *             the GPU need one each.
  * Sums are held in 32 bits within a thread and in 64 bits between them, in a
- * fixed order.  An infinity or a NaN in x makes its group of its image NaN and
+ * fixed order; values further than 1e18 from each other leave the range of
+ * their squares.  An infinity or a NaN in x makes its group of its image NaN and
  * no other.  With no images or no pixels nothing is written.
  * Errors: ASGD_EINVAL (null, unknown dtype or act, eps not > 0 and finite,
  * overlap), ASGD_ESHAPE (negative sizes, channels not a multiple of groups,
- * strides below channels or above 2^28 bytes, more than 2^30 pixels or 2^31
+ * strides below channels or above 2^28 bytes, more than 2^30 pixels or 2^24
  * groups in all),
  * ASGD_EALIGN, ASGD_EHIP. */
 typedef enum {

@@ -1851,7 +1851,7 @@ int check_group_norm(const char *name, const GroupNorm &q, uintptr_t tensors, ui
     if (q.ldx < q.channels || q.ldo < q.channels || q.lddy < q.channels) return fail(ASGD_ESHAPE, "%s: a pixel's stride is below its %d channels", name, q.channels);
     const double pixels = (double)q.batch * q.pixels;
     if (std::max(q.ldx, std::max(q.ldo, q.lddy)) > (1L << 28) / (long)dtype_size(q.dtype)) return fail(ASGD_ESHAPE, "%s: a pixel's stride is above 2^28 bytes", name);
-    if (q.pixels > 1 << 30 || (double)q.batch * q.groups >= 2147483648.0 || pixels * (double)std::max(q.ldx, std::max(q.ldo, q.lddy)) > 1e15)
+    if (q.pixels > 1 << 30 || (double)q.batch * q.groups > (double)(1 << 24) || pixels * (double)std::max(q.ldx, std::max(q.ldo, q.lddy)) > 1e15)
         return fail(ASGD_ESHAPE, "%s: sizes too large", name);
     const size_t es = dtype_size(q.dtype);
     if (((tensors | params) & (es - 1)) || (stats & 3) || ((uintptr_t)workspace & 15)) return fail(ASGD_EALIGN, "%s: misaligned buffer", name);

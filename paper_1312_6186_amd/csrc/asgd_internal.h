@@ -264,6 +264,10 @@ struct GroupNorm {
     int dtype, act, batch, pixels, channels, groups;
     long ldx, lddy, ldo;     // elements from pixel to pixel: of x, of dy (backward), of y or dx
 };
+// How a call with aligned tensors runs: values of a vector, and in slabs (threads > 0) whether vectors keep within a group, threads, VGPRs a thread for one
+// tensor, channels of a slab
+struct GroupNormPlan { int vector, uni, threads, regs, width; };
+GroupNormPlan group_norm_plan(const GroupNorm &q, bool bwd);
 size_t group_norm_ws(int batch, int pixels, int channels, int groups, int dtype);   // bytes of workspace, for both directions
 int launch_group_norm_fwd(const GroupNorm &q, const void *x, const void *gamma, const void *beta, void *y, float *mean, float *rstd, float eps, void *ws,
                           hipStream_t s);

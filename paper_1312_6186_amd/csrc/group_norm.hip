@@ -5,15 +5,17 @@
 //   dz = dy * act'(z),  A_c = sum_p dz,  B_c = sum_p dz * h   (of each image and channel)
 //   dx = rstd * (gamma_c * dz - (sum_g gamma A) / M - h * (sum_g gamma B) / M),  dbeta = sum_n A,  dgamma = sum_n B
 //
-// Bound by memory; the statistics stand between the first read of a value and its second one.  Here the tensor is read twice: a pass that
-// leaves sums of each image, chunk of pixels and channel, a small one that adds them up, and a pass that writes the result.
+// Bound by memory; the statistics stand between the first use of a value and its second one.  Where the groups of an image fit a workgroup's registers it
+// keeps them there (slabs: one read, one write); elsewhere the tensor is read twice (chunks: a pass that leaves sums of each image, chunk of pixels and
+// channel, a small one that adds them up, and a pass that writes the result).  us, slabs / chunks, in bf16: forward 256 images x 3025 pixels x 96 channels
+// 74 / 105 (both tensors at the rate of a copy 57), backward 143 / 173 (86, with an exponential twice a value, 73 of arithmetic), 128 x 729 x 256 42 / 63 (28).
 //
 // Sums.  A thread owns a vector of channels and strides over pixels, in 32 bits: forward about a value of its own (the first it reads),
 // which keeps the digits of values far from zero.  Sums of different threads meet in 64 bits, where sum x^2 / M - mean^2 loses nothing that
-// matters.  The order is fixed by the sizes alone.
+// matters.  The order is fixed by the sizes and the tensors' alignment alone.
 //
 // Which side of zero a ReLU's input was on is decided exactly, for the given mean and rstd: z > 0 is x > t (x < t where gamma < 0) with
-// t = mean - beta / (rstd * gamma), formed in 64 bits once per thread and channel and rounded to the next value in 32 bits that no x lies between.
+// t = mean - beta / (rstd * gamma), formed in 64 bits once a workgroup and channel and rounded to the next value in 32 bits that no x lies between.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -306,7 +308,7 @@ __device__ __forceinline__ void group_sums(const GnShape &s, const FastDiv &dcg,
 
 __global__ __launch_bounds__(kTeamThreads) void gn_fwd_stats_kernel(GnShape s, FastDiv dcg, const double *part, int team, float eps, float *mean, float *rstd)
 {
-    const unsigned i = (blockIdx.x * blockDim.x + threadIdx.x) / (unsigned)team;
+    const unsigned i = blockIdx.x * (blockDim.x / (unsigned)team) + threadIdx.x / (unsigned)team;
     group_sums(s, dcg, part, i, team, [](int) { return 1.0; }, [&](double a, double b) ASGD_INLINE {
         const float2 st = group_stats(a, b, (double)s.P * s.cg, eps);
         mean[i] = st.x;
@@ -436,7 +438,7 @@ __global__ __launch_bounds__(kThreads) void gn_param_grads_kernel(const double *
 template <typename T>
 __global__ __launch_bounds__(kTeamThreads) void gn_bwd_stats_kernel(GnShape s, FastDiv dcg, const double *part, const T *gamma, int team, float2 *coef)
 {
-    const unsigned i = (blockIdx.x * blockDim.x + threadIdx.x) / (unsigned)team;
+    const unsigned i = blockIdx.x * (blockDim.x / (unsigned)team) + threadIdx.x / (unsigned)team;
     group_sums(s, dcg, part, i, team, [&](int c) ASGD_INLINE { return gamma ? (double)ldf(&gamma[c]) : 1.0; }, [&](double a, double b) ASGD_INLINE {
         const double M = (double)s.P * s.cg;
         coef[i] = make_float2((float)(a / M), (float)(b / M));
@@ -758,8 +760,8 @@ __global__ __launch_bounds__(kSlabThreads) void gn_bwd_slab_kernel(GnSlab s, con
 // ---- host side
 
 // Chunks of pixels of 16 to 128 KiB of a tensor, small ones only as far as it takes 1024 workgroups (four a CU): what a workgroup does once (the constants
-// of its channels, the sums of its threads) is as much as 10 KiB take.  us, least 32 KiB and 2048 workgroups / as here:
-// CHUNKFIGS
+// of its channels, the sums of its threads) is as much as 10 KiB take.  us with at most 64, 128 and 256 KiB: backward 256 x 3025 x 96 bf16 177, 173, 178, 128 x
+// 729 x 256 61.6 each, forward 1 x 500000 x 64 47.3, 47.3, 46.4.
 void gn_chunks(int batch, int pixels, int channels, int dtype, int &chunks, int &pc)
 {
     const long bytes = (long)channels * (long)dtype_size(dtype);
@@ -794,7 +796,7 @@ bool gn_shape(const GroupNorm &q, int V, GnShape &s)
     s.dcbs = make_fastdiv((uint32_t)s.cbs);
     s.dchunks = make_fastdiv((uint32_t)s.chunks);
     s.dbx = make_fastdiv((uint32_t)s.bx);
-    return (double)s.N * s.chunks * s.cbs < 2147483648.0 && (double)s.N * s.G < 2147483648.0;
+    return (double)s.N * s.chunks * s.cbs * kThreads < 4e9;   // a launch has fewer than 2^32 threads
 }
 
 // Threads for the sums of one image and group: 64 where they have up to eight entries each, up to a whole workgroup.
@@ -861,7 +863,7 @@ template <int N> SlabPlan plan_slab(const GroupNorm &q, int vector, bool bwd, co
                 while (i < N && regs[i] < need) ++i;
                 if (i == N || (double)(regs[i] / (V * es / 4)) * rows * ld * es >= 2147483648.0) continue;   // offsets of all turns
                 const double total = (double)((q.channels + width - 1) / width) * q.batch;
-                if (total >= 1e9) continue;
+                if (total * threads >= 4e9) continue;   // a launch has fewer than 2^32 threads
                 const double us = slab_us(bwd, q.act, es, threads, need, width * es, total, (double)q.pixels * width * es);
                 if (best.V && us >= best_us) continue;
                 best_us = us; best_width = width;
@@ -933,6 +935,14 @@ size_t group_norm_ws(int batch, int pixels, int channels, int groups, int dtype)
     int chunks, pc;
     gn_chunks(batch, pixels, channels, dtype, chunks, pc);
     return round256((size_t)batch * chunks * channels * 16) + round256((size_t)batch * groups * 8);
+}
+
+GroupNormPlan group_norm_plan(const GroupNorm &q, bool bwd)
+{
+    const int V = gn_vector(q.dtype, q.channels, 0, q.ldx | q.lddy | q.ldo);
+    const SlabPlan p = bwd ? plan_slab(q, V, true, kBwdRegs) : plan_slab(q, V, false, kFwdRegs);
+    if (!p.V) return GroupNormPlan{V, 0, 0, 0, 0};
+    return GroupNormPlan{p.V, p.uni, p.threads, p.regs, p.s.width};
 }
 
 int launch_group_norm_fwd(const GroupNorm &q, const void *x, const void *gamma, const void *beta, void *y, float *mean, float *rstd, float eps, void *ws,

@@ -1,7 +1,7 @@
 """Group normalisation through the C ABI against the formulas in 64 bits.
 
-Tolerances.  A thread sums at most 64 values of a channel in 32 bits in these sizes (2^-18 of the sum of magnitudes at worst, taken twice: 2^-17); sums of
-threads meet in 64 bits.  Each fp32 operation rounds by 2^-24 relative, a store to a type by eps / 2 of it, and the hardware's exp2 and reciprocal by about
+Tolerances.  A thread sums at most 144 values in 32 bits (143 x 2^-24 < 2^-16.8 of the sum of their magnitudes at worst), forward about one of them, from which
+they are at most twice as far as from their mean on average: SUM = 2^-15.  Sums of threads meet in 64 bits.  Each fp32 operation rounds by 2^-24 relative, a store to a type by eps / 2 of it, and the hardware's exp2 and reciprocal by about
 2^-23, the exponent z log2(e) by |z| 2^-24."""
 import ctypes
 import math
@@ -16,6 +16,7 @@ from paper_1312_6186_amd import binding as B
 DEV = "cuda:0"
 TDT = {B.F32: torch.float32, B.BF16: torch.bfloat16}
 EPS = 1e-5
+SUM = 2.0 ** -15
 vp = ctypes.c_void_p
 
 
@@ -35,6 +36,7 @@ def test_bad_arguments_are_refused():
         assert call(dt=5) == B.EINVAL and call(act=3) == B.EINVAL and call(act=-1) == B.EINVAL
         assert call(n=-1) == B.ESHAPE and call(p=-1) == B.ESHAPE and call(c=0) == B.ESHAPE and call(g=0) == B.ESHAPE and call(g=3) == B.ESHAPE and call(g=32) == B.ESHAPE
         assert call(ldx=15) == B.ESHAPE and call(p=(1 << 30) + 1) == B.ESHAPE and call(n=1 << 30, g=4) == B.ESHAPE
+        assert call(n=(1 << 22) + 1, p=0, g=4) == B.ESHAPE and call(ldx=(1 << 26) + 1) == B.ESHAPE and call(ldx=(1 << 27) + 1, dt=B.BF16) == B.ESHAPE
         assert call(x=0) == B.EINVAL and call(ws=0) == B.EINVAL
         assert call(x=(1 << 20) + 2) == B.EALIGN and call(x=(1 << 20) + 1, dt=B.BF16) == B.EALIGN and call(gamma=(1 << 12) + 2) == B.EALIGN
         assert call(mean=(1 << 14) + 2) == B.EALIGN and call(ws=(1 << 16) + 8) == B.EALIGN
@@ -63,12 +65,72 @@ def test_workspace_sizes():
     assert B.asgd_group_norm_workspace_bytes(-1, 9, 16, 4, B.F32) == 0 and B.asgd_group_norm_workspace_bytes(1, 9, 16, 4, 9) == 0
 
 
+class _Call(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("dtype", "act", "batch", "pixels", "channels", "groups")] + [(n, ctypes.c_long) for n in ("ldx", "lddy", "ldo")]
+
+
+class _Plan(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("vector", "uni", "threads", "regs", "width")]
+
+
+def _plan(dtype, act, n, p, c, g, bwd):
+    """Internal function, by its mangled name."""
+    f = B.lib()["_ZN4asgd15group_norm_planERKNS_9GroupNormEb"]
+    f.argtypes, f.restype = [ctypes.POINTER(_Call), ctypes.c_bool], _Plan
+    return f(ctypes.byref(_Call(dtype, act, n, p, c, g, c, c, c)), bwd)
+
+
+# images, pixels, channels, groups that between them take every kernel for slabs
+SLABS = [(1, 1, 2, 1), (1, 1, 2, 2), (1, 1, 4, 4), (1, 1, 8, 1), (1, 1, 12, 1), (1, 1, 258, 2), (1, 1, 516, 4), (1, 7, 258, 2), (1, 13, 258, 2), (1, 17, 114, 2),
+         (1, 17, 228, 4), (1, 18, 114, 2), (1, 29, 132, 4), (1, 33, 114, 2), (1, 33, 228, 4), (1, 36, 114, 2), (1, 66, 114, 2), (1, 85, 24, 1), (1, 145, 124, 4),
+         (1, 205, 20, 4), (1, 261, 8, 1), (1, 340, 24, 1), (1, 341, 12, 1), (1, 355, 24, 1), (1, 392, 12, 1), (1, 445, 12, 1), (1, 457, 36, 4), (1, 528, 8, 1),
+         (1, 598, 24, 1), (1, 645, 16, 1), (1, 706, 12, 1), (1, 920, 10, 2), (1, 1038, 2, 1), (1, 1048, 16, 1), (1, 1388, 12, 1), (1, 1395, 6, 1), (1, 1549, 24, 1),
+         (1, 1554, 6, 1), (1, 1591, 12, 1), (1, 2052, 2, 1), (1, 2057, 4, 4), (1, 2594, 8, 1), (2, 1021, 12, 1), (9, 92, 224, 32), (9, 134, 64, 32), (9, 194, 192, 32),
+         (9, 309, 224, 32), (40, 1, 64, 32), (40, 1, 160, 32), (40, 1, 256, 32), (40, 8, 288, 32), (40, 10, 144, 16), (40, 261, 64, 32), (150, 12, 176, 16),
+         (150, 65, 516, 4)]
+
+
+def test_slabs_of_every_kind_are_among_the_cases():
+    kinds, threads, ragged = set(), set(), set()
+    for n, p, c, g in SLABS:
+        for dtype in (B.F32, B.BF16):
+            for bwd in (False, True):
+                q = _plan(dtype, B.ACT_RELU, n, p, c, g, bwd)
+                if q.threads:
+                    assert q.width <= q.threads and q.width % q.vector == 0 and (q.width == c or q.width % (c // g) == 0) and q.uni == ((c // g) % q.vector == 0)
+                    rows = q.threads // (q.width // q.vector)
+                    per = q.vector * (2 if dtype == B.BF16 else 4) // 4
+                    assert -(-p // rows) * per <= q.regs                    # an image's pixels fit the registers
+                    kinds.add((dtype, bwd, q.vector, q.uni, q.regs))
+                    threads.add((dtype, bwd, q.threads))
+                    ragged.add((dtype, bwd, c > q.width and c % q.width != 0))
+    for dtype in (B.F32, B.BF16):
+        for bwd, regs in ((False, (8, 16, 32, 72)), (True, (8, 16, 36, 72))):
+            for vector, uni in ((4, 1), (4, 0), (2, 1), (2, 0)) if dtype == B.F32 else ((8, 1), (4, 1), (4, 0)):
+                for r in regs:
+                    assert (dtype, bwd, vector, uni, r) in kinds, (dtype, bwd, vector, uni, r)
+            assert {(dtype, bwd, t) for t in (256, 512, 1024)} <= threads and (dtype, bwd, True) in ragged
+
+
+# Calls (type, activation, images, pixels, channels, groups, backward) with the us by chunks and in slabs
+WAYS = [(B.F32, 1, 8, 784, 8, 2, False, 9.6, 4.6), (B.BF16, 1, 256, 3025, 96, 8, False, 105.0, 74.3), (B.F32, 1, 128, 1024, 32, 8, True, 23.7, 15.7),
+        (B.BF16, 1, 128, 729, 256, 32, True, 63.2, 42.2), (B.BF16, 2, 256, 3025, 96, 8, True, 173.3, 142.6), (B.F32, 1, 14, 3404, 14, 2, True, 14.7, 21.8),
+        (B.BF16, 1, 33, 7120, 192, 32, True, 111.9, 228.8)]
+
+
+def test_calls_go_the_faster_way():
+    for dtype, act, n, p, c, g, bwd, chunks, slabs in WAYS:
+        assert (_plan(dtype, act, n, p, c, g, bwd).threads > 0) == (slabs < chunks), (dtype, act, n, p, c, g, bwd)
+
+
 # ---- on the GPU
 # images, pixels, channels, groups, columns behind the channels, element the tensors start at
 CASES = [(1, 1, 1, 1, 0, 0), (2, 1, 8, 2, 0, 0), (1, 3, 8, 8, 0, 0), (3, 7, 5, 5, 0, 0), (2, 49, 20, 4, 4, 0), (2, 50, 37, 1, 0, 0), (1, 2500, 96, 8, 0, 0),
          (4, 169, 384, 32, 0, 0), (2, 9, 4096, 16, 0, 0), (2, 5, 513, 27, 7, 0), (1, 4000, 8, 2, 0, 0), (130, 36, 16, 4, 0, 0), (3, 1000, 24, 2, 8, 0),
          (2, 300, 32, 4, 0, 1), (5, 121, 12, 3, 4, 3), (7, 64, 64, 32, 0, 0), (1, 257, 100, 20, 4, 0), (2, 33, 2056, 8, 0, 0)]
 IDS = ["x".join(map(str, c)) for c in CASES]
+SLAB_CASES = [(c + (0, 0), i % 3) for i, c in enumerate(SLABS)] + [(c + (0, 0), (i + 1) % 3) for i, c in enumerate(SLABS)]
+SLAB_IDS = ["x".join(map(str, c[:4])) + "-%d" % a for c, a in SLAB_CASES]
 
 
 def _tensor(rows, c, ld, shift, dtype, gen, offset=0.0, scale=1.0, fill=9.0):
@@ -106,14 +168,14 @@ def _spread(t, n, p, c, g):   # [n][g] -> [n * p][c]
 
 def _check_fwd(x, y, mean, rstd, gamma, beta, n, p, c, g, act, dtype):
     m64, r64, sd = _ref_stats(x, n, p, c, g)
-    assert ((mean.double() - m64).abs() <= 2.0 ** -24 * m64.abs() + 2.0 ** -17 * sd + 1e-30).all()
-    assert ((rstd.double() / r64 - 1).abs() <= 2.0 ** -17).all()
+    assert ((mean.double() - m64).abs() <= 2.0 ** -24 * m64.abs() + SUM * sd + 1e-30).all()
+    assert ((rstd.double() / r64 - 1).abs() <= SUM).all()
     ga, be = (gamma.double() if gamma is not None else torch.ones(c, device=DEV, dtype=torch.float64)), (beta.double() if beta is not None else 0.0)
     m, r = _spread(m64, n, p, c, g), _spread(r64, n, p, c, g)
     h = (x.double() - m) * r
     z = h * ga + be
     ref = _act64(z, act)
-    tol = ga.abs() * (2.0 ** -17 * _spread(sd * r64, n, p, c, g) + h.abs() * 2.0 ** -17 + 2.0 ** -23 * (m * r).abs()) + 2.0 ** -22 * z.abs()
+    tol = ga.abs() * (SUM * _spread(sd * r64, n, p, c, g) + h.abs() * SUM + 2.0 ** -23 * (m * r).abs()) + 2.0 ** -22 * z.abs()
     if act == B.ACT_SILU:
         tol = 1.1 * tol + ref.abs() * 2.0 ** -20 * (1 + z.abs())
     tol = tol + torch.finfo(TDT[dtype]).eps / 2 * ref.abs() + 1e-30
@@ -126,6 +188,17 @@ def _check_fwd(x, y, mean, rstd, gamma, beta, n, p, c, g, act, dtype):
 @pytest.mark.parametrize("dtype", [B.F32, B.BF16])
 @pytest.mark.parametrize("case", CASES, ids=IDS)
 def test_forward(case, dtype, act):
+    _forward(case, dtype, act)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("case,act", SLAB_CASES, ids=SLAB_IDS)
+def test_slabs_forward(case, dtype, act):
+    _forward(case, dtype, act)
+
+
+def _forward(case, dtype, act):
     n, p, c, g, pad, shift = case
     gen = torch.Generator(device=DEV).manual_seed(1)
     ld = c + pad
@@ -173,9 +246,9 @@ def _ref_bwd(dy, x, gamma, beta, mean, rstd, n, p, c, g, act):
     dh = ga * dz
     m1, m2 = groups(dh), groups(dh * h)
     dx = r * (dh - m1 - h * m2)
-    t = 2.0 ** -21 * (dh.abs() + m1.abs() + (h * m2).abs()) + 2.0 ** -17 * (groups(dh.abs()) + h.abs() * groups((dh * h).abs()))
+    t = 2.0 ** -21 * (dh.abs() + m1.abs() + (h * m2).abs()) + SUM * (groups(dh.abs()) + h.abs() * groups((dh * h).abs()))
     t = t + ga.abs() * e + groups(ga.abs() * e) + h.abs() * groups(ga.abs() * e * h.abs())
-    return (dx, (dz * h).sum(0), dz.sum(0)), (r * t, 2.0 ** -17 * (dz * h).abs().sum(0) + (e * h.abs()).sum(0), 2.0 ** -17 * dz.abs().sum(0) + e.sum(0))
+    return (dx, (dz * h).sum(0), dz.sum(0)), (r * t, SUM * (dz * h).abs().sum(0) + (e * h.abs()).sum(0), SUM * dz.abs().sum(0) + e.sum(0))
 
 
 @pytest.mark.gpu
@@ -183,6 +256,17 @@ def _ref_bwd(dy, x, gamma, beta, mean, rstd, n, p, c, g, act):
 @pytest.mark.parametrize("dtype", [B.F32, B.BF16])
 @pytest.mark.parametrize("case", CASES, ids=IDS)
 def test_backward(case, dtype, act):
+    _backward(case, dtype, act)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("case,act", SLAB_CASES, ids=SLAB_IDS)
+def test_slabs_backward(case, dtype, act):
+    _backward(case, dtype, act)
+
+
+def _backward(case, dtype, act):
     n, p, c, g, pad, shift = case
     gen = torch.Generator(device=DEV).manual_seed(2)
     ld = c + pad
