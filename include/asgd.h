@@ -406,6 +406,8 @@ int asgd_accumulate(float *accum, const float *grads, size_t n, int first, void 
  *   workspace : device, asgd_group_norm_workspace_bytes(...) bytes, 16-byte
  *             aligned; its contents do not matter, and calls that may overlap on
  *             the GPU need one each.
+ * gamma, beta, mean, rstd, dgamma, dbeta and the workspace share no memory with
+ * each other or with the tensors.
  * Sums are held in 32 bits within a thread and in 64 bits between them, in a
  * fixed order; values further than 1e18 from each other leave the range of
  * their squares.  An infinity or a NaN in x makes its group of its image NaN and
@@ -413,7 +415,8 @@ int asgd_accumulate(float *accum, const float *grads, size_t n, int first, void 
  * Errors: ASGD_EINVAL (null, unknown dtype or act, eps not > 0 and finite,
  * overlap), ASGD_ESHAPE (negative sizes, channels not a multiple of groups,
  * strides below channels or above 2^28 bytes, more than 2^30 pixels or 2^24
- * groups in all),
+ * groups in all, or more partial sums than 32 bits count, which takes tensors
+ * of tens of GB),
  * ASGD_EALIGN, ASGD_EHIP. */
 typedef enum {
     ASGD_ACT_NONE = 0,
@@ -456,6 +459,7 @@ int asgd_group_norm_bwd(const void *dy, const void *x, const void *gamma, const 
  *   workspace : device, asgd_grad_norm_workspace_bytes(n_tensors) bytes, 16-byte
  *             aligned; written before it is read, so its contents do not matter.
  *             Calls that may overlap on the GPU need one each.
+ * norm and the workspace share no memory with each other or with the tensors.
  * Squares are summed in 64 bits, in a fixed order. */
 size_t asgd_grad_norm_workspace_bytes(int n_tensors);
 /* Errors: ASGD_EINVAL (null, negative count of tensors, unknown dtype),

@@ -1889,8 +1889,9 @@ int asgd_group_norm_fwd(const void *x, const void *gamma, const void *beta, void
     if (batch == 0 || pixels == 0) return ASGD_OK;
     if (!x || !y || !workspace) return fail(ASGD_EINVAL, "asgd_group_norm_fwd: null argument");
     if (bad_overlap(q, x, ldx, y)) return fail(ASGD_EINVAL, "asgd_group_norm_fwd: y overlaps x");
-    if (launch_group_norm_fwd(q, x, gamma, beta, y, mean, rstd, eps, workspace, static_cast<hipStream_t>(stream)) != 0)
-        return hip_fail(hipGetLastError(), "group normalisation kernels");
+    const int lrc = launch_group_norm_fwd(q, x, gamma, beta, y, mean, rstd, eps, workspace, static_cast<hipStream_t>(stream));
+    if (lrc == kTooLarge) return fail(ASGD_ESHAPE, "asgd_group_norm_fwd: sizes too large");
+    if (lrc != 0) return hip_fail(hipGetLastError(), "group normalisation kernels");
     return ASGD_OK;
 }
 
@@ -1910,8 +1911,9 @@ int asgd_group_norm_bwd(const void *dy, const void *x, const void *gamma, const 
     }
     if (!dy || !x || !mean || !rstd || !dx || !workspace) return fail(ASGD_EINVAL, "asgd_group_norm_bwd: null argument");
     if (bad_overlap(q, dy, lddy, dx) || bad_overlap(q, x, ldx, dx)) return fail(ASGD_EINVAL, "asgd_group_norm_bwd: dx overlaps dy or x");
-    if (launch_group_norm_bwd(q, dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, workspace, st) != 0)
-        return hip_fail(hipGetLastError(), "group normalisation kernels");
+    const int lrc = launch_group_norm_bwd(q, dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, workspace, st);
+    if (lrc == kTooLarge) return fail(ASGD_ESHAPE, "asgd_group_norm_bwd: sizes too large");
+    if (lrc != 0) return hip_fail(hipGetLastError(), "group normalisation kernels");
     return ASGD_OK;
 }
 

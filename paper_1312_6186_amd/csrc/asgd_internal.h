@@ -268,6 +268,7 @@ struct GroupNorm {
 // tensor, channels of a slab
 struct GroupNormPlan { int vector, uni, threads, regs, width; };
 GroupNormPlan group_norm_plan(const GroupNorm &q, bool bwd);
+constexpr int kTooLarge = -2;   // of the launches below: more chunks than they can count
 size_t group_norm_ws(int batch, int pixels, int channels, int groups, int dtype);   // bytes of workspace, for both directions
 int launch_group_norm_fwd(const GroupNorm &q, const void *x, const void *gamma, const void *beta, void *y, float *mean, float *rstd, float eps, void *ws,
                           hipStream_t s);

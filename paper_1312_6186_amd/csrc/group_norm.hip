@@ -796,7 +796,7 @@ bool gn_shape(const GroupNorm &q, int V, GnShape &s)
     s.dcbs = make_fastdiv((uint32_t)s.cbs);
     s.dchunks = make_fastdiv((uint32_t)s.chunks);
     s.dbx = make_fastdiv((uint32_t)s.bx);
-    return (double)s.N * s.chunks * s.cbs * kThreads < 4e9;   // a launch has fewer than 2^32 threads
+    return (double)s.N * s.chunks * s.cbs * kThreads < 4e9 && (double)s.chunks * s.cg < 2e9;   // threads of a launch, sums that a group's team counts in 32 bits
 }
 
 // Threads for the sums of one image and group: 64 where they have up to eight entries each, up to a whole workgroup.
@@ -969,7 +969,7 @@ int launch_group_norm_fwd(const GroupNorm &q, const void *x, const void *gamma, 
         return launch_ok();
     }
     GnShape s;
-    if (!gn_shape(q, V, s)) return -1;
+    if (!gn_shape(q, V, s)) return kTooLarge;
     double *part = static_cast<double *>(ws);
     float *own = reinterpret_cast<float *>(static_cast<char *>(ws) + round256((size_t)s.N * s.chunks * s.C * 16));   // where the caller wants none
     if (!mean) mean = own;
@@ -1015,7 +1015,7 @@ int launch_group_norm_bwd(const GroupNorm &q, const void *dy, const void *x, con
         return launch_ok();
     }
     GnShape s;
-    if (!gn_shape(q, V, s)) return -1;
+    if (!gn_shape(q, V, s)) return kTooLarge;
     float2 *coef = reinterpret_cast<float2 *>(static_cast<char *>(ws) + round256((size_t)s.N * s.chunks * s.C * 16));
     const unsigned blocks = (unsigned)s.N * s.chunks * s.cbs;
     by_vector(q.dtype, V, [&](auto t, auto v) {

@@ -48,6 +48,13 @@ def test_bad_arguments_are_refused():
     assert _fwd(n=0, x=0, y=0, ws=0) == B.OK and _fwd(p=0) == B.OK      # nothing to do
 
 
+def test_partial_sums_beyond_32_bits_are_refused():
+    wide = dict(c=1 << 16, n=1, x=1 << 40, ldx=1 << 16)
+    for pixels in (1 << 17, 1 << 18):   # a pixel is a chunk: 2^33 sums of a group, and 2^24 workgroups
+        assert _fwd(p=pixels, g=1 if pixels == 1 << 17 else 1 << 14, y=1 << 44, ldy=1 << 16, **wide) == B.ESHAPE and "too large" in B.asgd_last_error()
+        assert _bwd(p=pixels, g=1 if pixels == 1 << 17 else 1 << 14, dy=1 << 42, dx=1 << 44, lddy=1 << 16, lddx=1 << 16, **wide) == B.ESHAPE
+
+
 def test_overlapping_outputs_are_refused():
     x = 1 << 20
     for call, name in ((lambda **k: _fwd(x=x, **k), "y"), (lambda **k: _bwd(x=x, dy=1 << 22, **{("dx" if q == "y" else "lddx" if q == "ldy" else q): v for q, v in k.items()}), "dx")):
