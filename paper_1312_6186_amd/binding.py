@@ -311,17 +311,22 @@ def asgd_apply_update_adadelta(params, avg_sq_grad, avg_sq_step, grads, rho, eps
 
 
 class TensorList:
-    """Device pointers and element counts of a list of tensors, for callers that pass the same tensors again and again."""
+    """Device pointers and element counts of a list of contiguous tensors of one type, for callers that pass the same tensors again and again."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
         self.n = len(self.tensors)
+        if any(not t.is_contiguous() for t in self.tensors) or any(t.dtype != self.tensors[0].dtype for t in self.tensors):
+            raise ValueError("a list of tensors takes contiguous ones of one type")
         self.ptrs = (ctypes.c_void_p * self.n)(*[t.data_ptr() for t in self.tensors])
         self.counts = (ctypes.c_size_t * self.n)(*[t.numel() for t in self.tensors])
 
 
-def _tensors(ts):
-    return ts if isinstance(ts, TensorList) else TensorList(ts)
+def _tensors(ts, dtype):
+    r = ts if isinstance(ts, TensorList) else TensorList(ts)
+    if r.n and r.tensors[0].element_size() != (2 if dtype == BF16 else 4):
+        raise ValueError("the tensors' elements have another size than dtype's")
+    return r
 
 
 def asgd_grad_norm_workspace_bytes(n_tensors):
@@ -330,14 +335,14 @@ def asgd_grad_norm_workspace_bytes(n_tensors):
 
 def asgd_grad_norm(grads, dtype, norm, workspace, stream=None):
     """grads: a list of device tensors, or a TensorList of them."""
-    g = _tensors(grads)
+    g = _tensors(grads, dtype)
     _check(lib().asgd_grad_norm(g.ptrs, g.counts, g.n, dtype, _ptr(norm), _ptr(workspace), _stream(stream)))
 
 
 def asgd_clip_grads(grads, clipped, dtype, max_norm, norm, workspace, stream=None):
     """grads, clipped: lists of as many device tensors of the same sizes (or TensorLists); the same list for both clips in place."""
-    g = _tensors(grads)
-    c = g if clipped is grads else _tensors(clipped)
+    g = _tensors(grads, dtype)
+    c = g if clipped is grads else _tensors(clipped, dtype)
     if c.n != g.n or (c is not g and bytes(c.counts) != bytes(g.counts)):
         raise ValueError("asgd_clip_grads: the clipped tensors have other sizes than the gradients")
     _check(lib().asgd_clip_grads(g.ptrs, c.ptrs, g.counts, g.n, dtype, max_norm, _ptr(norm), _ptr(workspace), _stream(stream)))

@@ -100,6 +100,15 @@ def test_lists_of_other_sizes_are_refused():
         B.asgd_clip_grads([a, a], [a], B.F32, 1.0, None, None)
 
 
+def test_lists_of_strided_or_other_tensors_are_refused():
+    a = torch.zeros(8)
+    for bad in ([torch.zeros(16)[::2]], [torch.zeros(1).expand(8)], [a, torch.zeros(8, dtype=torch.bfloat16)], [torch.zeros(8, dtype=torch.bfloat16)]):
+        with pytest.raises(ValueError):
+            B.asgd_grad_norm(bad, B.F32, a, None)
+        with pytest.raises(ValueError):
+            B.asgd_clip_grads([torch.zeros(t.numel()) for t in bad], bad, B.F32, 1.0, None, None)
+
+
 # ---- on the GPU
 def _workspace(n):
     return torch.empty(B.asgd_grad_norm_workspace_bytes(n), dtype=torch.uint8, device=DEV).fill_(255)   # as NaN as it can be
