@@ -7,6 +7,7 @@ library has not been built, loading it raises: there is no fallback path.
 """
 import ctypes
 import os
+from array import array
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libasgd_mi355x.so")
@@ -130,7 +131,7 @@ def _ptr(t):
 def _stream(stream):
     if stream is None:
         import torch
-        stream = torch.cuda.current_stream()
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())   # 0.4 us; torch.cuda.current_stream() makes an object of it, 2.8 us
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -314,12 +315,13 @@ class TensorList:
     """Device pointers and element counts of a list of contiguous tensors of one type, for callers that pass the same tensors again and again."""
 
     def __init__(self, tensors):
-        self.tensors = list(tensors)
-        self.n = len(self.tensors)
-        if any(not t.is_contiguous() for t in self.tensors) or any(t.dtype != self.tensors[0].dtype for t in self.tensors):
+        import torch
+        self.tensors = ts = list(tensors)
+        self.n = len(ts)
+        if not all(map(torch.Tensor.is_contiguous, ts)) or len({t.dtype for t in ts}) > 1:
             raise ValueError("a list of tensors takes contiguous ones of one type")
-        self.ptrs = (ctypes.c_void_p * self.n)(*[t.data_ptr() for t in self.tensors])
-        self.counts = (ctypes.c_size_t * self.n)(*[t.numel() for t in self.tensors])
+        self._ptrs, self.sizes = array("Q", map(torch.Tensor.data_ptr, ts)), array("Q", map(torch.Tensor.numel, ts))
+        self.ptrs, self.counts = self._ptrs.buffer_info()[0], self.sizes.buffer_info()[0]
 
 
 def _tensors(ts, dtype):
@@ -343,7 +345,7 @@ def asgd_clip_grads(grads, clipped, dtype, max_norm, norm, workspace, stream=Non
     """grads, clipped: lists of as many device tensors of the same sizes (or TensorLists); the same list for both clips in place."""
     g = _tensors(grads, dtype)
     c = g if clipped is grads else _tensors(clipped, dtype)
-    if c.n != g.n or (c is not g and bytes(c.counts) != bytes(g.counts)):
+    if c.n != g.n or (c is not g and c.sizes != g.sizes):
         raise ValueError("asgd_clip_grads: the clipped tensors have other sizes than the gradients")
     _check(lib().asgd_clip_grads(g.ptrs, c.ptrs, g.counts, g.n, dtype, max_norm, _ptr(norm), _ptr(workspace), _stream(stream)))
 
