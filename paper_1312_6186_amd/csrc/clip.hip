@@ -26,6 +26,13 @@ constexpr int kTilePieces = 1024;
 // 1024, 1536 workgroups: 161, 144, 139; 62 M parameters updated with 512, 1024, 1536, 2048: 286, 272, 277, 283).
 constexpr int kClipBlocks = 1536, kUpdateBlocks = 1024;
 
+// Short gradients take one launch of one workgroup, up to so many tiles and elements: a launch less, but a tile (each 256 threads take one at a time) takes
+// 0.3 to 0.6 us.  us a call, two launches / one: norm of 1, 8, 16 full fp32 tiles 6.3 / 3.9, 6.3 / 4.4, 6.3 / 6.2, of 8 and 12 bf16 tensors of 100 elements 6.4 /
+// 5.8, 6.3 / 7.5; clipping 4 and 8 full fp32 tiles 7.1 / 5.3, 7.1 / 7.6, 6 and 8 fp32 tensors of 1000 7.1 / 6.8, 7.3 / 7.7, 4 and 6 bf16 tensors of 100 (parts of
+// pieces, element by element) 7.9 / 6.8, 8.1 / 9.1; an update of 100, 4096, 8192, 16384 parameters 7.2 / 4.8, 7.1 / 4.7, 7.2 / 5.5, 7.3 / 7.5.
+constexpr int kFewTiles = 8, kFewClipped16 = 4;   // kFewClipped16: tiles of 16-bit tensors that are clipped
+constexpr size_t kFewNorm = 32768, kFewClip = 16384, kFewUpdate = 12288;
+
 static inline uint64_t tensor_tiles(const void *p, size_t count, int es)
 {
     if (count == 0) return 0;
@@ -38,14 +45,14 @@ template <typename T> struct Piece {
     union { u32x4 u; T e[E]; };
 };
 
-// The four pieces of tile `tile` of tensor q that belong to this thread, elements outside the tensor as zeros.  body(piece, first element, whole).
+// The four pieces of tile `tile` of tensor q that belong to this thread (one of 256), elements outside the tensor as zeros.  body(piece, first element, whole).
 template <typename T, bool ONCE, class F> __device__ __forceinline__ void each_piece(const TensorTable &t, int q, unsigned tile, F &&body)
 {
     constexpr int E = Piece<T>::E;
     const uintptr_t addr = reinterpret_cast<uintptr_t>(t.in[q]);
     const long head = (long)(addr & 15) / (long)sizeof(T), count = (long)t.count[q], start = (long)tile * kTilePieces * E - head;
     const T *base = reinterpret_cast<const T *>(addr & ~(uintptr_t)15);
-    const long first = (long)tile * kTilePieces + threadIdx.x;
+    const long first = (long)tile * kTilePieces + (threadIdx.x & 255);
     Piece<T> v[4];
     if (start >= 0 && start + kTilePieces * E <= count) {   // a tile inside the tensor: all loads at once
 #pragma unroll
@@ -76,11 +83,16 @@ template <typename T, bool ONCE, class F> __device__ __forceinline__ void each_p
     }
 }
 
-// The sum of one double a thread over the 256 threads of a workgroup, the same in all of them.
-__device__ __forceinline__ double block_sum(double s, double (&lds)[4])
+__device__ __forceinline__ double wave_sum(double s)
 {
 #pragma unroll
     for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+    return s;
+}
+// The sum of one double a thread over the 256 threads of a workgroup, the same in all of them.
+__device__ __forceinline__ double block_sum(double s, double (&lds)[4])
+{
+    s = wave_sum(s);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
     __syncthreads();
     return (lds[0] + lds[1]) + (lds[2] + lds[3]);
@@ -115,6 +127,17 @@ __device__ __forceinline__ int tensor_of(const TensorTable &t, unsigned tile)   
     return lo;
 }
 
+template <typename T, bool ONCE> __device__ __forceinline__ void tile_squares(const TensorTable &t, int q, unsigned tile, double &s)
+{
+    each_piece<T, ONCE>(t, q, tile - t.start[q], [&](const Piece<T> &v, long, bool) ASGD_INLINE {
+#pragma unroll
+        for (int e = 0; e < Piece<T>::E; ++e) {
+            const double x = (double)ldf(&v.e[e]);
+            s = __builtin_fma(x, x, s);
+        }
+    });
+}
+
 template <typename T, bool ONCE> __global__ __launch_bounds__(256) void square_sums_kernel(TensorTable t, double *partials)
 {
     __shared__ double lds[4];
@@ -125,13 +148,7 @@ template <typename T, bool ONCE> __global__ __launch_bounds__(256) void square_s
         int q = tensor_of(t, begin);
         for (unsigned tile = begin; tile < end; ++tile) {
             while (tile >= t.start[q + 1]) ++q;
-            each_piece<T, ONCE>(t, q, tile - t.start[q], [&](const Piece<T> &v, long, bool) ASGD_INLINE {
-#pragma unroll
-                for (int e = 0; e < Piece<T>::E; ++e) {
-                    const double x = (double)ldf(&v.e[e]);
-                    s = __builtin_fma(x, x, s);
-                }
-            });
+            tile_squares<T, ONCE>(t, q, tile, s);
         }
     }
     s = block_sum(s, lds);
@@ -145,9 +162,27 @@ __global__ __launch_bounds__(256) void norm_kernel(const double *partials, int n
     if (threadIdx.x == 0) *norm = (float)__builtin_sqrt(s);
 }
 
-template <typename T> __global__ __launch_bounds__(256) void clip_kernel(TensorTable t, const double *partials, int n, float max_norm, float *norm)
+template <typename T> __device__ __forceinline__ void clip_tile(const TensorTable &t, int q, unsigned tile, const Factor &f)
 {
     constexpr int E = Piece<T>::E;
+    T *out = static_cast<T *>(t.out[q]);
+    const bool aligned = ((reinterpret_cast<uintptr_t>(t.in[q]) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
+    const long count = (long)t.count[q];
+    each_piece<T, false>(t, q, tile - t.start[q], [&](Piece<T> v, long at, bool whole) ASGD_INLINE {
+#pragma unroll
+        for (int e = 0; e < E; ++e) stf(&v.e[e], clipped(ldf(&v.e[e]), f));
+        if (whole && aligned) {
+            __builtin_nontemporal_store(v.u, reinterpret_cast<u32x4 *>(out + at));   // what is still to be read stays in the cache (164 us with ordinary stores, 144)
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (at + e >= 0 && at + e < count) out[at + e] = v.e[e];
+        }
+    });
+}
+
+template <typename T> __global__ __launch_bounds__(256) void clip_kernel(TensorTable t, const double *partials, int n, float max_norm, float *norm)
+{
     __shared__ double lds[4];
     const double squares = sum_partials(partials, n, lds);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)__builtin_sqrt(squares);
@@ -160,20 +195,36 @@ template <typename T> __global__ __launch_bounds__(256) void clip_kernel(TensorT
     for (unsigned tile = end; tile-- > begin;) {
         while (tile < t.start[q]) --q;
         if (same && t.in[q] == t.out[q]) continue;   // clipped in place by a factor of one
-        T *out = static_cast<T *>(t.out[q]);
-        const bool aligned = ((reinterpret_cast<uintptr_t>(t.in[q]) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
-        const long count = (long)t.count[q];
-        each_piece<T, false>(t, q, tile - t.start[q], [&](Piece<T> v, long at, bool whole) ASGD_INLINE {
-#pragma unroll
-            for (int e = 0; e < E; ++e) stf(&v.e[e], clipped(ldf(&v.e[e]), f));
-            if (whole && aligned) {
-                __builtin_nontemporal_store(v.u, reinterpret_cast<u32x4 *>(out + at));   // what is still to be read stays in the cache (164 us with ordinary stores, 144)
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (at + e >= 0 && at + e < count) out[at + e] = v.e[e];
-            }
-        });
+        clip_tile<T>(t, q, tile, f);
+    }
+}
+
+// Short gradients in one launch, by one workgroup: each 256 of its threads take a tile at a time.  The sums are those of the kernels above, bit for bit.
+template <typename T> __device__ __forceinline__ double few_squares(const TensorTable &t, double (&lds)[kFewTiles][4])
+{
+    const unsigned tiles = t.start[t.n], lane = threadIdx.x & 63;
+    for (unsigned tile = threadIdx.x >> 8; tile < tiles; tile += 4) {
+        double s = 0;
+        tile_squares<T, false>(t, tensor_of(t, tile), tile, s);
+        s = wave_sum(s);
+        if (lane == 0) lds[tile][(threadIdx.x >> 6) & 3] = s;
+    }
+    __syncthreads();
+    return wave_sum(lane < tiles ? (lds[lane][0] + lds[lane][1]) + (lds[lane][2] + lds[lane][3]) : 0.0);
+}
+template <typename T, bool CLIP> __global__ __launch_bounds__(1024) void few_tiles_kernel(TensorTable t, float max_norm, float *norm)
+{
+    __shared__ double lds[kFewTiles][4];
+    const double squares = few_squares<T>(t, lds);
+    if (norm && threadIdx.x == 0) *norm = (float)__builtin_sqrt(squares);
+    if constexpr (CLIP) {
+        const Factor f = clip_factor(squares, max_norm);
+        const bool same = !f.drop && f.f == 1.0;
+        for (unsigned tile = threadIdx.x >> 8; tile < t.start[t.n]; tile += 4) {
+            const int q = tensor_of(t, tile);
+            if (same && t.in[q] == t.out[q]) continue;
+            clip_tile<T>(t, q, tile, f);
+        }
     }
 }
 
@@ -244,6 +295,33 @@ __global__ __launch_bounds__(256) void clipped_update_scalar_kernel(float *w, fl
     }
 }
 
+// The same for few elements, by one workgroup, with the sums of few_tiles_kernel.
+template <int SNAP>
+__global__ __launch_bounds__(1024) void few_update_kernel(TensorTable t, float *w, float *v, const float *g, unsigned n, float lr, float mu, float wd,
+                                                          float max_norm, float *norm, void *copy)
+{
+    constexpr int K = (int)(kFewUpdate / 1024);
+    __shared__ double lds[kFewTiles][4];
+    float ww[K], vv[K], gg[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {   // on their way while the squares are added up
+        const unsigned i = threadIdx.x + k * 1024;
+        if (i < n) { ww[k] = w[i]; vv[k] = v[i]; gg[k] = g[i]; }
+    }
+    const double squares = few_squares<float>(t, lds);
+    if (norm && threadIdx.x == 0) *norm = (float)__builtin_sqrt(squares);
+    const Factor f = clip_factor(squares, max_norm);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const unsigned i = threadIdx.x + k * 1024;
+        if (i >= n) break;
+        update1(ww[k], vv[k], clipped(gg[k], f), lr, mu, wd);
+        v[i] = vv[k]; w[i] = ww[k];
+        if constexpr (SNAP == 1) static_cast<float *>(copy)[i] = ww[k];
+        if constexpr (SNAP == 2) static_cast<uint16_t *>(copy)[i] = (uint16_t)f32_to_bf16_bits(__float_as_uint(ww[k]));
+    }
+}
+
 // ---- host side
 
 size_t norm_partials(int n_tensors)
@@ -290,6 +368,20 @@ template <class F> static long each_table(const void *const *in, void *const *ou
     return first;
 }
 
+// Whether a call is for one workgroup.
+static bool few(const void *const *in, const size_t *counts, int n, int dtype, int most_tiles, size_t most)
+{
+    if (n > kTableTensors) return false;
+    uint64_t tiles = 0;
+    size_t total = 0;
+    for (int i = 0; i < n; ++i) {
+        if (counts[i] > most) return false;
+        tiles += tensor_tiles(in[i], counts[i], (int)dtype_size(dtype));
+        total += counts[i];
+    }
+    return tiles > 0 && tiles <= (uint64_t)most_tiles && total <= most;
+}
+
 // once: by non-temporal loads
 static long launch_square_sums(const void *const *grads, const size_t *counts, int n, int dtype, bool once, double *partials, hipStream_t s)
 {
@@ -307,6 +399,11 @@ bool norm_streams(size_t bytes) { return bytes > ((size_t)192 << 20); }
 
 int launch_grad_norm(const void *const *grads, const size_t *counts, int n, int dtype, float *norm, double *partials, hipStream_t s)
 {
+    if (few(grads, counts, n, dtype, kFewTiles, kFewNorm))
+        return each_table(grads, nullptr, counts, n, dtype, [&](const TensorTable &t, unsigned, long) {
+            if (dtype == kBF16) hipLaunchKernelGGL((few_tiles_kernel<bf16_t, false>), dim3(1), dim3(1024), 0, s, t, 0.f, norm);
+            else hipLaunchKernelGGL((few_tiles_kernel<float, false>), dim3(1), dim3(1024), 0, s, t, 0.f, norm);
+        }) < 0 ? -1 : 0;
     size_t bytes = 0;
     for (int i = 0; i < n; ++i) bytes += counts[i] * dtype_size(dtype);
     const long np = launch_square_sums(grads, counts, n, dtype, norm_streams(bytes), partials, s);
@@ -317,6 +414,11 @@ int launch_grad_norm(const void *const *grads, const size_t *counts, int n, int 
 
 int launch_clip(const void *const *grads, void *const *out, const size_t *counts, int n, int dtype, float max_norm, float *norm, double *partials, hipStream_t s)
 {
+    if (few(grads, counts, n, dtype, dtype == kBF16 ? kFewClipped16 : kFewTiles, kFewClip))
+        return each_table(grads, out, counts, n, dtype, [&](const TensorTable &t, unsigned, long) {
+            if (dtype == kBF16) hipLaunchKernelGGL((few_tiles_kernel<bf16_t, true>), dim3(1), dim3(1024), 0, s, t, max_norm, norm);
+            else hipLaunchKernelGGL((few_tiles_kernel<float, true>), dim3(1), dim3(1024), 0, s, t, max_norm, norm);
+        }) < 0 ? -1 : 0;
     const long np = launch_square_sums(grads, counts, n, dtype, false, partials, s);
     if (np < 0) return -1;
     if (np == 0) {
@@ -357,6 +459,13 @@ int launch_update_clipped(float *w, float *v, const float *g, size_t n, float lr
                           double *partials, hipStream_t s)
 {
     const void *grads[1] = {g};
+    if (few(grads, &n, 1, kF32, kFewTiles, kFewUpdate))
+        return each_table(grads, nullptr, &n, 1, kF32, [&](const TensorTable &t, unsigned, long) {
+            const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(1), dim3(1024), 0, s, t, w, v, g, (unsigned)n, lr, mu, wd, max_norm, norm, copy); };
+            if (!copy) go(few_update_kernel<0>);
+            else if (dst_dtype == kBF16) go(few_update_kernel<2>);
+            else go(few_update_kernel<1>);
+        }) < 0 ? -1 : 0;
     const long np = launch_square_sums(grads, &n, 1, kF32, false, partials, s);
     if (np < 0) return -1;
     if (!copy) return launch_update_clipped_t<0>(w, v, g, n, lr, mu, wd, max_norm, norm, nullptr, partials, (int)np, s);

@@ -294,6 +294,31 @@ def test_clipped_update_of_long_vectors(n):
     assert ((gc.double() - g.double() * f).abs() <= 2.0 ** -22 * (g.double() * f).abs()).all()
 
 
+# one workgroup or many: a push of up to 12288 elements, clipping of up to 16384, norms of up to 32768, of up to eight tiles each (four where 16 bits are clipped)
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes", [[12288], [12289], [16384], [16385], [32768], [32769], [3000, 17, 4096, 1, 900, 4100], [100] * 8, [100] * 9, [8192, 8192]])
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+def test_one_workgroup_and_many_agree(sizes, dtype):
+    n = sum(sizes)
+    w, v, g = _update_inputs(n, 9, 0)
+    whole = g.to(TDT[dtype])
+    views, outs = list(whole.split(sizes)), list(torch.empty_like(whole).split(sizes))
+    norms, ref = torch.zeros(3, device=DEV), _norm64(views)
+    m = float(np.float32(0.5 * ref))
+    B.asgd_grad_norm(views, dtype, norms[0:1], _workspace(len(views)))
+    B.asgd_clip_grads(views, outs, dtype, m, norms[1:2], _workspace(len(views)))
+    assert abs(norms[0].item() - ref) <= (2.0 ** -24 + 2.0 ** -40) * ref and norms[0].item() == norms[1].item()
+    tol = torch.finfo(TDT[dtype]).eps / 2 * (1 + 2.0 ** -20) + 2.0 ** -22
+    for a, o in zip(views, outs):
+        exact = a.double() * (m / ref)
+        assert ((o.double() - exact).abs() <= tol * exact.abs()).all()
+    if dtype == B.F32 and len(sizes) == 1:
+        w2, v2, c, c2 = w.clone(), v.clone(), torch.zeros(n, device=DEV), torch.zeros(n, device=DEV)
+        B.asgd_apply_update_clipped(w, v, whole, 0.05, 0.9, 1e-3, m, c, B.F32, norms[2:3], _workspace(1))
+        B.asgd_apply_update_snapshot(w2, v2, outs[0], 0.05, 0.9, 1e-3, c2, B.F32)
+        assert torch.equal(w, w2) and torch.equal(v, v2) and torch.equal(c, c2) and norms[2].item() == norms[1].item()
+
+
 @pytest.mark.gpu
 def test_a_dropped_push_moves_parameters_by_momentum_alone():
     w, v, g = _update_inputs(4097, 8, 0)
