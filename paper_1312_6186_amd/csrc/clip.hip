@@ -100,7 +100,13 @@ __device__ __forceinline__ double block_sum(double s, double (&lds)[4])
 __device__ __forceinline__ double sum_partials(const double *partials, int n, double (&lds)[4])
 {
     double s = 0;
-    for (int i = threadIdx.x; i < n; i += 256) s += partials[i];
+    for (int i = threadIdx.x; i < n; i += 256 * 6) {   // six at once: all there are of a table
+        double v[6];
+#pragma unroll
+        for (int u = 0; u < 6; ++u) v[u] = i + u * 256 < n ? partials[i + u * 256] : 0.0;
+#pragma unroll
+        for (int u = 0; u < 6; ++u) s += v[u];
+    }
     return block_sum(s, lds);
 }
 
