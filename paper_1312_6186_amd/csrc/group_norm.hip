@@ -412,25 +412,29 @@ __global__ __launch_bounds__(kThreads) void gn_bwd_sums_kernel(GnShape s, const 
 // dgamma and dbeta of four channels, 64 threads each over `entries` (images and chunks of them).
 __global__ __launch_bounds__(kThreads) void gn_param_grads_kernel(const double *part, long entries, int C, float *dgamma, float *dbeta)
 {
-    __shared__ double2 lds[kThreads];
+    __shared__ double2 lds[kThreads / 64][4];
     const int c = (int)blockIdx.x * 4 + ((int)threadIdx.x & 3);
     double2 t = make_double2(0, 0);
     if (c < C) {
-#pragma unroll 4
-        for (long j = threadIdx.x >> 2; j < entries; j += kThreads / 4) {
-            const double2 v = reinterpret_cast<const double2 *>(part)[(size_t)j * C + c];
-            t.x += v.x; t.y += v.y;
+        for (long j = threadIdx.x >> 2; j < entries; j += kThreads) {   // four at once
+            double2 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const long k = j + u * (kThreads / 4);
+                v[u] = k < entries ? reinterpret_cast<const double2 *>(part)[(size_t)k * C + c] : make_double2(0, 0);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) { t.x += v[u].x; t.y += v[u].y; }
         }
     }
-    lds[threadIdx.x] = t;
+#pragma unroll
+    for (int d = 32; d >= 4; d >>= 1) { t.x += __shfl_xor(t.x, d); t.y += __shfl_xor(t.y, d); }
+    if ((threadIdx.x & 63) < 4) lds[threadIdx.x >> 6][threadIdx.x & 3] = t;
     __syncthreads();
-    for (int d = kThreads / 2; d >= 4; d >>= 1) {
-        if ((int)threadIdx.x < d) { lds[threadIdx.x].x += lds[threadIdx.x + d].x; lds[threadIdx.x].y += lds[threadIdx.x + d].y; }
-        __syncthreads();
-    }
     if (threadIdx.x < 4 && c < C) {
-        if (dbeta) dbeta[c] = (float)lds[threadIdx.x].x;
-        if (dgamma) dgamma[c] = (float)lds[threadIdx.x].y;
+        for (int w = 1; w < kThreads / 64; ++w) { t.x += lds[w][threadIdx.x].x; t.y += lds[w][threadIdx.x].y; }
+        if (dbeta) dbeta[c] = (float)t.x;
+        if (dgamma) dgamma[c] = (float)t.y;
     }
 }
 
