@@ -23,7 +23,7 @@ namespace asgd {
 // vector: they start and end anywhere).  Each thread takes four pieces of a tile.
 constexpr int kTilePieces = 1024;
 // Workgroups of a pass.  Fewer leave memory waiting, more add the partial sums up more often (us, 161 tensors of 100 M elements in bf16 clipped with 512,
-// 1024, 1536 workgroups: 161, 144, 139; 62 M parameters updated with 512, 1024, 1536, 2048: 286, 272, 277, 283).
+// 1024, 1536, 2048 workgroups: 159, 140, 133, 136; 62 M parameters updated with 512, 1024, 1536, 2048: 280, 268, 275, 276).
 constexpr int kClipBlocks = 1536, kUpdateBlocks = 1024;
 
 // Short gradients take one launch of one workgroup, up to so many tiles and elements: a launch less, but a tile (each 256 threads take one at a time) takes
@@ -178,7 +178,7 @@ template <typename T> __device__ __forceinline__ void clip_tile(const TensorTabl
 #pragma unroll
         for (int e = 0; e < E; ++e) stf(&v.e[e], clipped(ldf(&v.e[e]), f));
         if (whole && aligned) {
-            __builtin_nontemporal_store(v.u, reinterpret_cast<u32x4 *>(out + at));   // what is still to be read stays in the cache (164 us with ordinary stores, 144)
+            __builtin_nontemporal_store(v.u, reinterpret_cast<u32x4 *>(out + at));   // what is still to be read stays in the cache (159 us with ordinary stores, 133)
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e)

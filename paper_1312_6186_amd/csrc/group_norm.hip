@@ -8,7 +8,7 @@
 // Bound by memory; the statistics stand between the first use of a value and its second one.  Where the groups of an image fit a workgroup's registers it
 // keeps them there (slabs: one read, one write); elsewhere the tensor is read twice (chunks: a pass that leaves sums of each image, chunk of pixels and
 // channel, a small one that adds them up, and a pass that writes the result).  us, slabs / chunks, in bf16: forward 256 images x 3025 pixels x 96 channels
-// 74 / 105 (both tensors at the rate of a copy 57), backward 143 / 173 (86, with an exponential twice a value, 73 of arithmetic), 128 x 729 x 256 42 / 63 (28).
+// 74 / 105 (both tensors at the rate of a copy 57), backward 144 / 173 (86, with an exponential twice a value, 73 of arithmetic), 128 x 729 x 256 41 / 62 (28).
 //
 // Sums.  A thread owns a vector of channels and strides over pixels, in 32 bits: forward about a value of its own (the first it reads),
 // which keeps the digits of values far from zero.  Sums of different threads meet in 64 bits, where sum x^2 / M - mean^2 loses nothing that
